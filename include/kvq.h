@@ -80,10 +80,12 @@ extern "C" {
 #define KVQ_ERR_CUDA_LAUNCH (-6)
 #define KVQ_ERR_DEVICE_TIMEOUT (-7)
 #define KVQ_ERR_STATIC_SCRATCH (-8) /* problem needs more scratch than the library's built-in buffer */
+#define KVQ_ERR_BAD_INPUT (-9)      /* a length, offset or page number in device memory was out of range (paged calls) */
 
 /* bits that kernels OR into *kvq_cache.status (never trap) */
 #define KVQ_STATUS_CAPACITY 1u       /* an append would exceed capacity_tokens; that sequence was skipped */
 #define KVQ_STATUS_DEVICE_TIMEOUT 2u /* a bounded device-side wait expired */
+#define KVQ_STATUS_BAD_INPUT 4u      /* paged calls: a length, offset or page number was out of range; see there */
 
 /* dtypes */
 #define KVQ_FP16 0
@@ -249,6 +251,89 @@ int kvq_quant_error(const kvq_config* cfg, const void* k, const void* v,
  * b_K > b_V; this is the form its preceding line implies.)  Both sums must be positive.
  */
 int kvq_bit_balance(double sum_k2, double sum_v2, double* bk_minus_bv);
+
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Paged cache: the same packed pages in a pool, named by a block table, for ragged batches of a serving engine.  (The paper
+ * has no counterpart; its quantizer, grouping and attention are those above.)
+ *
+ * Pool: pages [n_pages][n_kv_heads][page_bytes], an entry being one 128-token page of one KV head as above.  Tokens 128 i ..
+ * 128 i + 127 of sequence b live in pool page block_table[b * table_stride + i].  Keys are token-wise and not rotated by
+ * kvq_cache.k_signs; kb and vb are 2, 4 or 8; there is no residual window: other configurations are KVQ_ERR_UNSUPPORTED.
+ * capacity_tokens bounds the length of a sequence (the table has at least capacity_tokens / 128 columns); batch <= 1024.
+ *
+ * Ragged calls: cu (device, int32 [batch + 1], cu[0] = 0, not decreasing) gives the rows cu[b] .. cu[b + 1] - 1 of sequence b
+ * among the n_rows rows of the call's tensors.  They are the LAST cu[b + 1] - cu[b] of the seq_len[b] tokens that the sequence
+ * holds once the call's tokens are counted in: row i stands at position seq_len[b] - cu[b + 1] + i.  The library never changes
+ * seq_len, so that all layers share one.  Rows from cu[batch] on are padding (a captured graph's) and are left as they were.
+ *
+ * Everything in device memory is checked before it is used as an index.  A sequence with decreasing or too large offsets, more
+ * rows than tokens, a length beyond capacity_tokens (or the rotation's table, or with more than max_rows rows) is passed
+ * over: none of its rows is written.  A page number outside the pool makes the append leave out the tokens of that page, the read-back
+ * leave their rows as they were, and the attention's rows of that sequence undefined (another page is read in its place).  All
+ * of these set KVQ_STATUS_BAD_INPUT.  Different tokens of a call have to lie in different places; all calls are asynchronous on cuda_stream.
+ * ------------------------------------------------------------------------------------------------------------------- */
+typedef struct {
+  void* pages;                /* device; 16-byte aligned; pool as above */
+  int32_t n_pages;            /* pages in the pool, >= 1 */
+  const int32_t* block_table; /* device */
+  int64_t table_stride;       /* entries between the rows of two sequences, >= capacity_tokens / 128 */
+  const int32_t* seq_len;     /* device [batch]: tokens per sequence, those of the call counted in */
+  int32_t* status;            /* device, one word of KVQ_STATUS_* bits */
+} kvq_paged_cache;            /* one per layer; block_table and seq_len may be shared by layers */
+
+/* Rotation of query and key rows by position p, with r = rotary_dim: channels (i, i + r/2) (or (2 i, 2 i + 1) where interleaved)
+ * become (a cos - b sin, b cos + a sin) with cos = cos[p][i], sin = sin[p][i]; channels from r on stay.  Every product and sum is an
+ * individually rounded fp32 operation; queries are then rounded to in_dtype, keys are quantized from the fp32 values. */
+typedef struct {
+  const float* cos;           /* device [n_positions][rotary_dim / 2], 16-byte aligned */
+  const float* sin;
+  int32_t n_positions;
+  int32_t rotary_dim;         /* multiple of 16, at most head_dim */
+  int32_t interleaved;        /* 0 or 1 */
+} kvq_rope;
+
+/*
+ * Rotate the call's keys (and queries), quantize its keys and values (App. B.1 quantizer per group, as kvq_quantize_append) and
+ * store them in their pages.
+ *   k, v: device, in_dtype, element (row, head, d) at offset row * kv_stride_row + head * kv_stride_head + d (in elements; each
+ *     row of head_dim channels 16-byte aligned, e.g. slices of one projection output).
+ *   q, q_out: both NULL, or device, in_dtype: q with strides of its own, q_out [n_rows][n_q_heads][head_dim] contiguous.  q_out may
+ *     be q where q is contiguous too.  Needs rope.
+ *   rope: NULL stores the keys as they are.
+ * Not safe to call concurrently on the same pages.
+ */
+int kvq_paged_append(const kvq_config* cfg, const kvq_paged_cache* cache, const void* k, const void* v,
+                     int64_t kv_stride_row, int64_t kv_stride_head, const int32_t* cu, int32_t n_rows,
+                     const kvq_rope* rope, const void* q, int64_t q_stride_row, int64_t q_stride_head, void* q_out,
+                     void* cuda_stream);
+
+/*
+ * Attention of the call's rows over the paged cache (App. A.1: S = Q K^T / sqrt(d), A = softmax(S), A V): a row at position p
+ * attends to the tokens t <= p that are also t > p - window or t < sinks (window 0: to all t <= p) - a sliding window whose
+ * first `sinks` tokens stay visible.  Pages that no row of the call sees are not read: their table entries may be anything.
+ *   q, out: device, [n_rows][n_q_heads][head_dim] contiguous, 16-byte aligned (q in_dtype, out out_dtype: KVQ_FP16/BF16/FP32).
+ *   max_rows: no sequence has more rows in this call (1: a decoding step); sizes the workspace and chooses the kernel.  Up to
+ *     n_q_heads / n_kv_heads * max_rows = 8 (row, head) pairs per KV head are served by the kernel behind kvq_decode_attention where it
+ *     is built for the configuration, everything else by one that makes 16-bit tiles of the pages for the tensor cores; a batch
+ *     of long chunks and single tokens is faster as two calls.
+ *   softmax_scale <= 0 selects 1/sqrt(head_dim).
+ *   workspace: device scratch of at least kvq_paged_workspace_bytes(), 16-byte aligned, contents arbitrary.  Calls that may
+ *     overlap on the GPU need separate ones.
+ */
+int kvq_paged_workspace_bytes(const kvq_config* cfg, int32_t max_rows, size_t* out);
+int kvq_paged_attention(const kvq_config* cfg, const kvq_paged_cache* cache, const void* q, const int32_t* cu,
+                        int32_t n_rows, int32_t max_rows, int32_t window, int32_t sinks, void* out, int32_t out_dtype,
+                        float softmax_scale, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Read the tokens of the call's rows back: x^ = fmaf(code, s, z) rounded to in_dtype (App. B.1: A^ = scale * Q).
+ *   k_out, v_out: device, in_dtype, [n_rows][n_kv_heads][head_dim] contiguous, 16-byte aligned; either may be NULL.
+ */
+int kvq_paged_dequantize(const kvq_config* cfg, const kvq_paged_cache* cache, const int32_t* cu, int32_t n_rows,
+                         void* k_out, void* v_out, void* cuda_stream);
+
+/* kvq_check_status for a paged cache; KVQ_ERR_BAD_INPUT where that bit is set. */
+int kvq_paged_check_status(const kvq_paged_cache* cache, void* cuda_stream);
 
 /* Synchronises cuda_stream, reads *cache->status and returns KVQ_OK, KVQ_ERR_CAPACITY,
  * KVQ_ERR_DEVICE_TIMEOUT or KVQ_ERR_CUDA_LAUNCH (a CUDA error surfaced by the sync). */

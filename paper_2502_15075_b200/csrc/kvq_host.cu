@@ -13,6 +13,8 @@ namespace {
 bool is_bits(int b) { return b == 1 || b == 2 || b == 3 || b == 4 || b == 6 || b == 8 || b == 16; }
 bool is_group(int g) { return g == 32 || g == 64 || g == 128; }
 
+}  // namespace
+
 int make_geom(const kvq_config* cfg, Geom* out) {
   if (!cfg) return KVQ_ERR_INVALID_ARG;
   if (cfg->batch <= 0 || cfg->n_kv_heads <= 0 || cfg->n_q_heads <= 0) return KVQ_ERR_INVALID_ARG;
@@ -52,6 +54,8 @@ int make_geom(const kvq_config* cfg, Geom* out) {
   *out = g;
   return KVQ_OK;
 }
+
+namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -406,6 +410,7 @@ int kvq_check_status(const kvq_cache* cache, void* cuda_stream) {
   if (cudaStreamSynchronize(s) != cudaSuccess) return KVQ_ERR_CUDA_LAUNCH;
   if (st & KVQ_STATUS_DEVICE_TIMEOUT) return KVQ_ERR_DEVICE_TIMEOUT;
   if (st & KVQ_STATUS_CAPACITY) return KVQ_ERR_CAPACITY;
+  if (st & KVQ_STATUS_BAD_INPUT) return KVQ_ERR_BAD_INPUT;
   return KVQ_OK;
 }
 
@@ -422,6 +427,7 @@ const char* kvq_strerror(int code) {
     case KVQ_ERR_STATIC_SCRATCH:
       return "this configuration needs more split scratch than the library's built-in 8 MiB buffer; "
              "use kvq_decode_attention with a caller-provided workspace";
+    case KVQ_ERR_BAD_INPUT: return "a length, offset or page number in device memory is out of range";
     default: return "unknown kvq error";
   }
 }

@@ -27,6 +27,9 @@ inline cudaError_t launch_dependent(void (*kern)(P...), dim3 grid, unsigned thre
   return e;
 }
 
+// Checks a configuration and works out its geometry (kvq_host.cu).
+int make_geom(const kvq_config* cfg, Geom* out);
+
 int launch_quantize_append(const Geom& g, const CachePtrs& c, const void* k_new, const void* v_new,
                            int64_t sb, int64_t sh, int64_t st, int t_new, cudaStream_t stream);
 

@@ -1,0 +1,73 @@
+// What the kernels of the paged cache share: its pointers, the checks of everything that comes from device memory, and the pages that a
+// sequence's rows see under a sliding window with first tokens that stay visible.
+#pragma once
+
+#include "kvq_internal.h"
+
+namespace kvq {
+
+// A paged cache and a ragged call on it (device memory).
+struct Paged {
+  uint8_t* pages;            // [n_pool][Hkv][page_bytes]
+  const int32_t* table;      // pool page of tokens 128 i .. of sequence b: table[b * table_stride + i]
+  long long table_stride;
+  const int32_t* seq_len;    // [B], the call's tokens counted in
+  const int32_t* cu;         // [B + 1]
+  uint32_t* status;
+  int n_pool, n_rows;
+  int max_rows, window, sinks;      // attention only (window 0: none)
+};
+
+struct RopeArgs { const float *cos, *sin; int n_positions, half, interleaved; };      // half: rotary_dim / 2, 0 without a rotation
+
+// The rows of a sequence in a call: rows first .. first + rows - 1 are the last `rows` of its n tokens.
+struct SeqRows { int n, rows, first; };
+
+// ... of sequence b, checked; `rows` is 0 where something is out of range (then `bad` says so).
+__device__ __forceinline__ SeqRows seq_rows(const Paged& p, int b, int limit, int max_rows, bool& bad) {
+  const int c0 = p.cu[b], c1 = p.cu[b + 1], n = p.seq_len[b];
+  bad = c0 < 0 || c1 < c0 || c1 > p.n_rows || n < 0 || n > limit;
+  bad = bad || c1 - c0 > n || c1 - c0 > max_rows;
+  return SeqRows{bad ? 0 : n, bad ? 0 : c1 - c0, bad ? 0 : c0};
+}
+
+// The sequence of row i: the number of ends cu[1 ..] at or below it.  The whole warp asks for the same row.
+__device__ __forceinline__ int sequence_of(const int32_t* cu, int B, int i, int lane) {
+  int lo = 0, len = B;                           // the answer is in lo .. lo + len - 1 (or B, which the caller's check finds out)
+  while (len > 32) {
+    const int step = (len + 31) >> 5, at = lo + lane * step;            // first entries of up to 32 pieces
+    const bool below = at < lo + len && cu[at] <= i;                    // (cu[b] <= i for the answer b and all before it)
+    const int k = __popc(__ballot_sync(0xffffffffu, below));
+    const int piece = k > 0 ? k - 1 : 0, end = lo + len;
+    lo += piece * step;
+    len = min(step, end - lo);
+  }
+  const bool passed = lane < len && cu[lo + lane + 1] <= i;
+  return min(lo + __popc(__ballot_sync(0xffffffffu, passed)), B - 1);
+}
+
+// Pool page of logical page `page` of sequence b, or -1 (outside the pool).
+__device__ __forceinline__ int pool_page(const Paged& p, int b, int page) {
+  const int id = p.table[(long long)b * p.table_stride + page];
+  return (unsigned)id < (unsigned)p.n_pool ? id : -1;
+}
+
+// Logical pages that tokens of positions p0 .. p1 see (p0 <= p1, rows of a call): `first` pages from the sequence's start, then those
+// from page `low` on; `count` in all.  Page i of them is logical page i < first ? i : i + skip.
+struct SeenPages {
+  int count, first, skip;
+  __host__ __device__ __forceinline__ int logical(int i) const { return i < first ? i : i + skip; }
+};
+__host__ __device__ __forceinline__ SeenPages seen_pages(int p0, int p1, int window, int sinks) {
+  const int reach = p0 - window + 1;                                    // first token that the window of the earliest row holds
+  const int low = window > 0 && reach > 0 ? reach >> 7 : 0;
+  const int first = min((int)(((unsigned)sinks + 127u) >> 7), low);
+  return SeenPages{(p1 >> 7) + 1 - low + first, first, low - first};
+}
+
+int launch_paged_append(const Geom& g, const Paged& p, const void* k, const void* v, int64_t kv_row, int64_t kv_head,
+                        const RopeArgs& rope, const void* q, int64_t q_row, int64_t q_head, void* q_out, cudaStream_t stream);
+int launch_paged_dequantize(const Geom& g, const Paged& p, void* k_out, void* v_out, cudaStream_t stream);
+int launch_paged_plain(const Geom& g, const Paged& p, const void* q, void* out, int out_dtype, float scale_log2e, cudaStream_t stream);
+
+}  // namespace kvq

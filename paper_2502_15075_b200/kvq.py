@@ -23,7 +23,7 @@ _lib = ctypes.CDLL(LIB_PATH)
 
 KVQ_FP16, KVQ_BF16, KVQ_FP32 = 0, 1, 2
 PAGE_TOKENS = 128
-STATUS_CAPACITY, STATUS_DEVICE_TIMEOUT = 1, 2
+STATUS_CAPACITY, STATUS_DEVICE_TIMEOUT, STATUS_BAD_INPUT = 1, 2, 4
 
 
 class kvq_config(ctypes.Structure):
@@ -36,6 +36,16 @@ class kvq_cache(ctypes.Structure):
     _fields_ = [("pages", ctypes.c_void_p), ("k_tail", ctypes.c_void_p),
                 ("seq_len", ctypes.c_void_p), ("status", ctypes.c_void_p), ("k_signs", ctypes.c_void_p),
                 ("kv_win", ctypes.c_void_p)]
+
+
+class kvq_paged_cache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("block_table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("seq_len", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
+class kvq_rope(ctypes.Structure):
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("n_positions", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
 
 _P = ctypes.POINTER
@@ -75,6 +85,15 @@ _lib.kvq_debug_decode_plan.argtypes = [_P(kvq_config), ctypes.c_int32] + [ctypes
 _lib.kvq_debug_decode_ring.argtypes = [_P(kvq_config), ctypes.c_int32, ctypes.c_void_p]
 _lib.kvq_debug_decode_windows.argtypes = [_P(kvq_config), ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p]
 _lib.kvq_debug_divide.argtypes = [ctypes.c_void_p] * 3 + [ctypes.c_int32, ctypes.c_void_p]
+_lib.kvq_paged_append.argtypes = [_P(kvq_config), _P(kvq_paged_cache), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64,
+                                  ctypes.c_void_p, ctypes.c_int32, _P(kvq_rope), ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64,
+                                  ctypes.c_void_p, ctypes.c_void_p]
+_lib.kvq_paged_workspace_bytes.argtypes = [_P(kvq_config), ctypes.c_int32, _P(ctypes.c_size_t)]
+_lib.kvq_paged_attention.argtypes = [_P(kvq_config), _P(kvq_paged_cache), ctypes.c_void_p, ctypes.c_void_p] + [ctypes.c_int32] * 4 + [
+    ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+_lib.kvq_paged_dequantize.argtypes = [_P(kvq_config), _P(kvq_paged_cache), ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
+                                      ctypes.c_void_p, ctypes.c_void_p]
+_lib.kvq_paged_check_status.argtypes = [_P(kvq_paged_cache), ctypes.c_void_p]
 _lib.kvq_check_status.argtypes = [_P(kvq_cache), ctypes.c_void_p]
 _lib.kvq_strerror.argtypes = [ctypes.c_int]
 _lib.kvq_strerror.restype = ctypes.c_char_p
@@ -82,13 +101,15 @@ for _f in ("kvq_page_bytes", "kvq_cache_bytes", "kvq_workspace_bytes", "kvq_quan
            "kvq_decode_attention", "kvq_decode_attention_static", "kvq_dequantize", "kvq_check_status",
            "kvq_quant_error", "kvq_bit_balance", "kvq_debug_decode_generic", "kvq_debug_decode_stall",
            "kvq_debug_decode_impl", "kvq_debug_decode_stall_impl", "kvq_debug_decode_plan", "kvq_debug_decode_ring", "kvq_debug_decode_windows",
-           "kvq_debug_divide", "kvq_workspace_bytes_rows", "kvq_decode_attention_rows"):
+           "kvq_debug_divide", "kvq_workspace_bytes_rows", "kvq_decode_attention_rows", "kvq_paged_append", "kvq_paged_workspace_bytes",
+           "kvq_paged_attention", "kvq_paged_dequantize", "kvq_paged_check_status"):
     getattr(_lib, _f).restype = ctypes.c_int
 
 EXPORTS = ("kvq_layout_version", "kvq_page_bytes", "kvq_cache_bytes", "kvq_workspace_bytes",
            "kvq_quantize_append", "kvq_decode_attention", "kvq_decode_attention_static", "kvq_dequantize",
            "kvq_check_status", "kvq_strerror", "kvq_quant_error", "kvq_bit_balance", "kvq_workspace_bytes_rows",
-           "kvq_decode_attention_rows", "kvq_window_bytes")
+           "kvq_decode_attention_rows", "kvq_window_bytes", "kvq_paged_append", "kvq_paged_workspace_bytes", "kvq_paged_attention",
+           "kvq_paged_dequantize", "kvq_paged_check_status")
 STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -389,8 +410,126 @@ def kvq_debug_divide(n: torch.Tensor, d: torch.Tensor):
     return q
 
 
-def kvq_check_status(cache: Cache, stream: Optional[torch.cuda.Stream] = None) -> int:
-    """Synchronises the stream and returns the library's status code (0 = ok)."""
+# ----------------------------------------------------------------------------
+# Paged cache (ragged batches; see kvq.h)
+# ----------------------------------------------------------------------------
+class PagedCache:
+    """A layer's pool of packed pages with the block table and the lengths of a batch (torch tensors) and the POD handed to the library."""
+
+    def __init__(self, cfg: kvq_config, n_pages: Optional[int] = None, pages: Optional[torch.Tensor] = None,
+                 block_table: Optional[torch.Tensor] = None, seq_len: Optional[torch.Tensor] = None, device="cuda"):
+        """pages: the pool, a contiguous uint8 CUDA tensor [n_pages, n_kv_heads, page bytes] (or n_pages: a new one).
+        block_table: int32 CUDA tensor [batch, >= capacity_tokens / 128], rows of any stride; seq_len: contiguous int32 [batch].
+        All may be shared with other layers' caches; what is not given is made here (table entries -1, lengths 0).
+        They are kept, not copied: replace none of them, write into them."""
+        self.cfg = cfg
+        page_bytes, columns = kvq_page_bytes(cfg), cfg.capacity_tokens // PAGE_TOKENS
+        if pages is None:
+            assert n_pages is not None, "a pool: pages, or n_pages to make one"
+            pages = torch.zeros((n_pages, cfg.n_kv_heads, page_bytes), dtype=torch.uint8, device=device)
+        assert pages.is_cuda and pages.dtype == torch.uint8 and pages.is_contiguous()
+        assert pages.dim() == 3 and tuple(pages.shape[1:]) == (cfg.n_kv_heads, page_bytes)
+        if block_table is None:
+            block_table = torch.full((cfg.batch, columns), -1, dtype=torch.int32, device=pages.device)
+        assert block_table.is_cuda and block_table.dtype == torch.int32 and block_table.dim() == 2
+        assert block_table.shape[0] == cfg.batch and block_table.shape[1] >= columns and block_table.stride(1) == 1
+        if seq_len is None:
+            seq_len = torch.zeros(cfg.batch, dtype=torch.int32, device=pages.device)
+        assert seq_len.is_cuda and seq_len.dtype == torch.int32 and seq_len.is_contiguous() and tuple(seq_len.shape) == (cfg.batch,)
+        assert pages.device == block_table.device == seq_len.device
+        self.pages, self.block_table, self.seq_len = pages, block_table, seq_len
+        self.status = torch.zeros(1, dtype=torch.int32, device=pages.device)
+        stride = block_table.stride(0) if cfg.batch > 1 else max(columns, block_table.stride(0))
+        self.c = kvq_paged_cache(pages.data_ptr(), pages.shape[0], block_table.data_ptr(), stride, seq_len.data_ptr(), self.status.data_ptr())
+
+
+class Rope:
+    """Tables of the rotation by position: cos, sin contiguous fp32 CUDA tensors [positions, rotary_dim / 2]."""
+
+    def __init__(self, cos: torch.Tensor, sin: torch.Tensor, interleaved: bool = False):
+        assert cos.is_cuda and cos.device == sin.device and cos.dim() == 2 and cos.shape == sin.shape
+        assert cos.dtype == torch.float32 and sin.dtype == torch.float32 and cos.is_contiguous() and sin.is_contiguous()
+        self.cos, self.sin = cos, sin
+        self.c = kvq_rope(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)))
+
+
+def _ragged(cfg: kvq_config, cache: PagedCache, cu: torch.Tensor, *tensors: torch.Tensor):
+    """The checks that all paged calls share: the offsets, and everything on the pool's device."""
+    assert cu.dtype == torch.int32 and cu.dim() == 1 and cu.shape[0] == cfg.batch + 1 and cu.is_contiguous()
+    device = cache.pages.device
+    assert cu.device == device and all(t.device == device for t in tensors), "all tensors on the pool's device"
+
+
+def _on_device(cache: PagedCache):
+    """The library launches on the current device: it has to be the pool's."""
+    assert cache.pages.device.index == torch.cuda.current_device(), "the pool's device has to be the current one (torch.cuda.device)"
+
+
+def kvq_paged_append(cfg: kvq_config, cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor,
+                     rope: Optional[Rope] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None):
+    """k, v [rows, Hkv, D] of the config's dtype with identical strides (e.g. slices of one projection output), last dim contiguous;
+    cu int32 [batch + 1].  rope: rotate k (and q, to q_out [rows, Hq, D] contiguous) by position first."""
+    n = k.shape[0]
+    strides = k.stride()
+    assert k.dim() == 3 and k.shape == v.shape and strides == v.stride() and strides[2] == 1
+    assert k.shape[1] == cfg.n_kv_heads and k.shape[2] == cfg.head_dim and v.dtype == k.dtype and _dtype_code(k.dtype) == cfg.in_dtype
+    _ragged(cfg, cache, cu, k, v)
+    _on_device(cache)
+    q_ptr = out_ptr = None
+    q_strides = (0, 0)
+    assert (q is None) == (q_out is None), "q and q_out together"
+    if q is not None:
+        assert q.dim() == 3 and q.shape == (n, cfg.n_q_heads, cfg.head_dim) and q.stride(2) == 1 and q.dtype == k.dtype
+        assert q_out.shape == q.shape and q_out.is_contiguous() and q_out.dtype == q.dtype and q.device == q_out.device == k.device
+        q_ptr, out_ptr, q_strides = q.data_ptr(), q_out.data_ptr(), q.stride()
+    if rope is not None:
+        assert rope.cos.device == k.device
+    _check(_lib.kvq_paged_append(ctypes.byref(cfg), ctypes.byref(cache.c), k.data_ptr(), v.data_ptr(), strides[0], strides[1],
+                                 cu.data_ptr(), n, None if rope is None else ctypes.byref(rope.c), q_ptr, q_strides[0], q_strides[1],
+                                 out_ptr, _stream_ptr(stream)), "kvq_paged_append")
+
+
+def kvq_paged_workspace_bytes(cfg: kvq_config, max_rows: int) -> int:
+    out = ctypes.c_size_t()
+    _check(_lib.kvq_paged_workspace_bytes(ctypes.byref(cfg), int(max_rows), ctypes.byref(out)), "kvq_paged_workspace_bytes")
+    return out.value
+
+
+def kvq_paged_attention(cfg: kvq_config, cache: PagedCache, q: torch.Tensor, cu: torch.Tensor, out: torch.Tensor,
+                        workspace: torch.Tensor, max_rows: int, window: int = 0, sinks: int = 0, softmax_scale: float = 0.0,
+                        stream: Optional[torch.cuda.Stream] = None):
+    """q, out [rows, Hq, D] contiguous (q of the config's dtype, out fp16/bf16/fp32); cu int32 [batch + 1]; no sequence has more
+    than max_rows rows; workspace: uint8 CUDA tensor of at least kvq_paged_workspace_bytes(cfg, max_rows).  A row at position p sees the
+    tokens t <= p with t > p - window or t < sinks (window 0: all of them)."""
+    assert q.dim() == 3 and q.shape[1] == cfg.n_q_heads and q.shape[2] == cfg.head_dim and out.shape == q.shape
+    assert q.is_contiguous() and out.is_contiguous() and workspace.is_contiguous() and _dtype_code(q.dtype) == cfg.in_dtype
+    _ragged(cfg, cache, cu, q, out, workspace)
+    _on_device(cache)
+    _check(_lib.kvq_paged_attention(ctypes.byref(cfg), ctypes.byref(cache.c), q.data_ptr(), cu.data_ptr(), q.shape[0], int(max_rows),
+                                    int(window), int(sinks), out.data_ptr(), _dtype_code(out.dtype), float(softmax_scale),
+                                    workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+           "kvq_paged_attention")
+
+
+def kvq_paged_dequantize(cfg: kvq_config, cache: PagedCache, cu: torch.Tensor, k_out: Optional[torch.Tensor],
+                         v_out: Optional[torch.Tensor], stream: Optional[torch.cuda.Stream] = None):
+    """k_out, v_out [rows, Hkv, D] contiguous of the config's dtype (or None): the tokens of the call's rows in 16 bits."""
+    given = [t for t in (k_out, v_out) if t is not None]
+    _ragged(cfg, cache, cu, *given)
+    _on_device(cache)
+    for t in given:
+        assert t.dim() == 3 and t.is_contiguous() and _dtype_code(t.dtype) == cfg.in_dtype
+        assert t.shape[0] == given[0].shape[0] and tuple(t.shape[1:]) == (cfg.n_kv_heads, cfg.head_dim)
+    _check(_lib.kvq_paged_dequantize(ctypes.byref(cfg), ctypes.byref(cache.c), cu.data_ptr(), given[0].shape[0] if given else 0,
+                                     k_out.data_ptr() if k_out is not None else None,
+                                     v_out.data_ptr() if v_out is not None else None, _stream_ptr(stream)), "kvq_paged_dequantize")
+
+
+def kvq_check_status(cache, stream: Optional[torch.cuda.Stream] = None) -> int:
+    """Synchronises the stream and returns the library's status code (0 = ok) of a Cache or a PagedCache."""
+    if isinstance(cache, PagedCache):
+        return _lib.kvq_paged_check_status(ctypes.byref(cache.c), _stream_ptr(stream))
     return _lib.kvq_check_status(ctypes.byref(cache.c), _stream_ptr(stream))
 
 
