@@ -35,7 +35,7 @@ size_t flat_workspace_bytes(const Geom& g) {
 
 // Id of a launch: the words that count a stream's finished partials carry it, so that neither stale workspace
 // contents nor an earlier call's counts are ever taken for this call's.  Starts at a clock value, never 0.
-static unsigned long long next_call_id() {
+unsigned long long next_call_id() {
   static std::atomic<unsigned long long> counter{
       ((unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() << 20) | 1ull};
   unsigned long long v = counter.fetch_add(1, std::memory_order_relaxed);

@@ -4,6 +4,7 @@
 #include <type_traits>
 
 #include "kvq_decode_mma.cuh"
+#include "kvq_paged.cuh"
 
 namespace kvq {
 namespace mma {
@@ -19,13 +20,14 @@ struct SmemLayout {
 __host__ __device__ constexpr int weight_block_bytes(int nh) { return 512 * nh; }
 __host__ __device__ constexpr int reduction_bytes(int ngv) { return 4 * (8 * ngv * 8 + (8 + 4 + 8) * 4); }   // per warp: p z sums (64 bits), maxima, scale limit, l
 __host__ __device__ inline int chan_stage_bytes(int D, int nh) { return nh * 2 * (D / 16) * 32 * 4 + 64; }
-__host__ __device__ inline SmemLayout smem_layout(int page_bytes, int stages, int batch, int D, int nh, int ngv, bool chan) {
+// prefs: words per sequence (two prefixes, pages and pages + stream gaps; a paged call also keeps its tokens, rows and first row).
+__host__ __device__ inline SmemLayout smem_layout(int page_bytes, int stages, int batch, int D, int nh, int ngv, bool chan, int prefs = 2) {
   SmemLayout s;
   s.page_stride = (page_bytes + 127) & ~127;
   s.ring_bytes = s.page_stride * stages;
   s.bar_off = s.ring_bytes;
   s.pref_off = s.bar_off + 16 * 8 * 2;                      // up to 32 barriers: (full, empty[, ready]) per stage
-  s.misc_off = (s.pref_off + 2 * (batch + 1) * 4 + 15) & ~15;      // two prefixes: pages, and pages + stream gaps
+  s.misc_off = (s.pref_off + prefs * (batch + 1) * 4 + 15) & ~15;
   s.w_off = s.misc_off + 64;
   s.red_off = s.w_off + 2 * ngv * 4 * weight_block_bytes(nh);
   s.chan_off = s.red_off + reduction_bytes(ngv);
@@ -36,9 +38,9 @@ __host__ __device__ inline SmemLayout smem_layout(int page_bytes, int stages, in
 // Stages of the ring for `minb` resident CTAs per SM, or fewer than two where a configuration does not fit.
 // Deeper rings do not help, and more bytes in flight cost DRAM efficiency: at most four stages and 54 KB (K4V4, 17 KB pages, 8B
 // shape: four stages 97.9 us, three 89.8 us; K4V2, 13 KB pages: four 76.8 us, three 77.3 us).
-inline int ring_stages(const Geom& g, int nh, int ngv, bool chan, int minb) {
+inline int ring_stages(const Geom& g, int nh, int ngv, bool chan, int minb, int prefs = 2) {
   const int budget = (227 * 1024) / minb - 1024;            // shared memory per CTA
-  int stages = (budget - smem_layout(0, 0, g.B, g.D, nh, ngv, chan).total) /
+  int stages = (budget - smem_layout(0, 0, g.B, g.D, nh, ngv, chan, prefs).total) /
                (((g.page_bytes + 127) & ~127) + (chan ? chan_stage_bytes(g.D, nh) : 0));
   if (stages > 4) stages = 4;
   if (stages > 2 && stages * ((g.page_bytes + 127) & ~127) > 54 * 1024) stages = 3;
@@ -142,10 +144,11 @@ constexpr int kFlushPages = 128;           // fold the int32 value accumulators 
 
 // The query values a lane needs as MMA operand: head hb (a (row, head) pair when several rows are served), channels
 // 16 r + 4 tid + {0..3} for every slot r; heads >= G are zero.  First as they are in memory, so that they can be on their way ...
+// first: the sequence's first query row of the call, G: its (row, head) pairs per KV head.
 template <int D>
-__device__ __forceinline__ void load_q_raw(const Geom& g, const uint16_t* __restrict__ q, int b, int h, int hb, int tid, uint2 (&raw)[D / 16]) {
-  const int Gq = g.G, G = g.G * g.rows;
-  const uint16_t* qrow = q + (((size_t)b * g.rows + hb / Gq) * g.Hq + (size_t)h * Gq + hb % Gq) * D;
+__device__ __forceinline__ void load_q_raw(const Geom& g, const uint16_t* __restrict__ q, size_t first, int G, int h, int hb, int tid, uint2 (&raw)[D / 16]) {
+  const int Gq = g.G;
+  const uint16_t* qrow = q + ((first + hb / Gq) * g.Hq + (size_t)h * Gq + hb % Gq) * D;
 #pragma unroll
   for (int r = 0; r < D / 16; ++r) {
     raw[r] = make_uint2(0u, 0u);
@@ -448,12 +451,17 @@ __device__ __forceinline__ void window_partial(const Geom& g, const uint16_t* wi
 // 16,384 tokens K8V2 101.6 -> 88.4; 4 x 8 streams of 4,000 tokens 22.5 -> 18.0.
 // The two token rows of a lane share every fp32 operation on logits and weights that has a packed form: two 70B-shaped layers at 128k
 // tokens, step 256 -> 251 us, 8B shape 181 -> 179.
+// PAGED: pages of a pool named by a block table, ragged query rows, a sliding window whose first tokens stay visible (kvq_paged.cuh).  A
+// stream is then the pages that its sequence's rows see, and its number of rows its own (g.rows: the most of any).
 constexpr int kConsumerWarps = 4;
-template <int D, int KB, int VB, int KAXIS, int NGK, int NGV, int NH, int MINB, bool WIN>
+struct NotPaged {};
+template <bool PAGED> struct PagedArg { using type = NotPaged; };
+template <> struct PagedArg<true> { using type = Paged; };
+template <int D, int KB, int VB, int KAXIS, int NGK, int NGV, int NH, int MINB, bool WIN, bool PAGED = false>
 __global__ void __launch_bounds__((kConsumerWarps + 1) * 32, MINB)
 decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1, float* __restrict__ ws,
                   int s_cap, int stages, void* __restrict__ out, int out_dtype, unsigned long long call_id,
-                  unsigned long long wait_ns, long long skip_x) {
+                  unsigned long long wait_ns, long long skip_x, typename PagedArg<PAGED>::type pa) {
   constexpr int NW = kConsumerWarps;
   constexpr int NR = D / 16;                // 16-channel register slots per key row
   constexpr int KS32 = D / 32;              // k-steps of an 8-bit MMA over the channels
@@ -481,10 +489,12 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
   static_assert(MT % FPBV == 0, "value m-tiles come in groups that share a byte");
 
   extern __shared__ __align__(128) uint8_t smem[];
-  const SmemLayout sl = smem_layout(g.page_bytes, stages, g.B, D, NH, NGV, KAXIS == 1);
+  static_assert(!PAGED || (KAXIS == 0 && !WIN), "paged caches have token-wise keys and no residual window");
+  const SmemLayout sl = smem_layout(g.page_bytes, stages, g.B, D, NH, NGV, KAXIS == 1, PAGED ? 5 : 2);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + sl.bar_off);   // full[0..stages), empty[0..stages)
   int* sPref = reinterpret_cast<int*>(smem + sl.pref_off);
   int* sVPref = sPref + (g.B + 1);                                   // the same prefix with GAP more per stream
+  [[maybe_unused]] int* sSeq = sVPref + (g.B + 1);                   // PAGED: tokens, rows, first row per sequence
   // [0] CTA that takes the segment's window, [1] abort flag, [2] published count, [3] CTAs that count themselves, [4..7] share ends, [8..9] segment
   // slot / partials, [10] CTAs taking part, [11..13] cursor, [14] weighted shares, [15] free.  A word has one meaning and one place that sets it
   // (besides the abort flag's start): whoever reads it is a barrier away from that place on both sides.
@@ -499,6 +509,8 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
   // Several query rows per head (g.rows > 1) are served as virtual heads: row r of head j is virtual head
   // r * Gq + j, with its own causal limit on the tokens it may see.
   const int B = g.B, Hkv = g.Hkv, Gq = g.G, G = g.G * g.rows;
+  int pa_sinks = 0;
+  if constexpr (PAGED) pa_sinks = pa.sinks;
 
   // ---- plan, all of it on warp 0 (the others wait at one barrier): pages per sequence, prefix over the batch,
   // this CTA's share of the pages and the stream its first page lies in
@@ -517,13 +529,27 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
   }
   begin_after_predecessor();
   // the queries, which a stream's start waits for, come to L2 while the split is worked out
-  for (long long i = ((long long)blockIdx.x * blockDim.x + tid_) * 64; i < (long long)B * g.rows * g.Hq * D; i += (long long)gridDim.x * blockDim.x * 64)
+  long long q_rows = (long long)B * g.rows;
+  if constexpr (PAGED) q_rows = pa.n_rows;
+  for (long long i = ((long long)blockIdx.x * blockDim.x + tid_) * 64; i < q_rows * g.Hq * D; i += (long long)gridDim.x * blockDim.x * 64)
     asm volatile("prefetch.global.L2 [%0];" ::"l"(q + i));
   if (warp == 0) {
     int carry = 0, vcarry = 0, pmax = 0;
     for (int base = 0; base < B; base += 32) {
       const int i = base + lane;
-      const int pages = (i < B) ? (paged_len(c.seq_len, i, g.capacity, g.R) + kPageTokens - 1) >> 7 : 0;
+      int pages = 0;
+      if constexpr (PAGED) {
+        if (i < B) {
+          bool bad;
+          const SeqRows s = seq_rows(pa, i, g.capacity, g.rows, bad);
+          if (bad) atomicOr(c.status, KVQ_STATUS_BAD_INPUT);
+          if (s.rows > 0) pages = seen_pages(s.n - s.rows, s.n - 1, pa.window, pa.sinks).count;
+          sSeq[3 * i] = s.n; sSeq[3 * i + 1] = s.rows; sSeq[3 * i + 2] = s.first;
+        }
+        __syncwarp();
+      } else {
+        pages = (i < B) ? (paged_len(c.seq_len, i, g.capacity, g.R) + kPageTokens - 1) >> 7 : 0;
+      }
       pmax = max(pmax, pages);
       int v = pages * Hkv;
       int vv = v > 0 ? v + GAP * Hkv : 0;
@@ -549,7 +575,8 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
   }
   __syncthreads();
   // a sequence without pages has no CTA of its own: its output rows are zero, or the attention over its residual window
-  for (int bb = blockIdx.x; bb < B; bb += gridDim.x) {
+  // (paged: a sequence without pages has no rows)
+  for (int bb = blockIdx.x; !PAGED && bb < B; bb += gridDim.x) {
     if (sPref[bb + 1] == sPref[bb] && (!WIN || clamped_len(c.seq_len, bb, g.capacity) == 0)) {
       for (int i = tid_; i < g.rows * g.Hq * D; i += blockDim.x) {
         const size_t oi = (size_t)bb * g.rows * g.Hq * D + i;
@@ -608,8 +635,72 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
   volatile int* n_published = sMisc + 2;      // count returned for the partial just published
   const unsigned long long id40 = (call_id & 0xFFFFFFFFFFull) ? (call_id & 0xFFFFFFFFFFull) : 1ull;
 
+  // What a sequence's rows see of its pages.
+  [[maybe_unused]] auto seen_of = [&](int bb) {
+    if constexpr (PAGED) {
+      const int n = sSeq[3 * bb], rows = sSeq[3 * bb + 1];
+      return seen_pages(n - rows, n - 1, pa.window, pa.sinks);
+    }
+    return SeenPages{0, 0, 0};
+  };
   // =========================================================== producer warp
-  if (KAXIS == 0 && warp == NW) {
+  // Paged: the lanes hold the pool pages of the next 32 pages of the stream, so that a page costs no look-up on its way.
+  if constexpr (PAGED) {
+    if (warp == NW) {
+      int it = 0, stage = 0, ids = 0, ids_page = 0, ids_b = -1;
+      uint32_t phase = 1;                // parity of the previous round of `empty`
+      bool ok = true;
+      const uint64_t policy = l2_evict_first_policy();
+      SeenPages seen{0, 0, 0};
+      for (int x = x_lo; x < x_hi; ++x, ++it) {
+        if (b != ids_b || page < ids_page || page >= ids_page + 32) {
+          if (b != ids_b) seen = seen_of(b);
+          ids_b = b; ids_page = page;
+          ids = page + lane < pages_b ? pool_page(pa, b, seen.logical(page + lane)) : 0;
+          if (ids < 0) {                 // outside the pool: another page is read in its place
+            atomicOr(c.status, KVQ_STATUS_BAD_INPUT);
+            ids = 0;
+          }
+          __syncwarp();
+        }
+        const int id = __shfl_sync(FULL, ids, page - ids_page);
+        if (it >= stages) {
+          bool free_ = true;
+          if (lane == 0) free_ = mbar_wait(bar0 + 8 * (stages + stage), phase, wait_ns) && !*abort_flag;
+          ok = __all_sync(FULL, free_);
+          if (!ok) break;
+        }
+        if (lane == 0 && x != skip_x) {          // (skip_x: test hook - a page that never arrives makes the consumers' bounded wait expire)
+          const uint32_t fb = bar0 + 8 * stage;
+          mbar_expect_tx(fb, (uint32_t)g.page_bytes);
+          bulk_load(ring + stage * sl.page_stride, pa.pages + ((size_t)id * Hkv + h) * (size_t)g.page_bytes, (uint32_t)g.page_bytes, fb, policy);
+        }
+        __syncwarp();
+        if (++stage == stages) { stage = 0; phase ^= 1; }
+        if (++page == pages_b) {
+          page = 0;
+          if (++h == Hkv) {
+            h = 0;
+            do { ++b; } while (b < B && sPref[b + 1] == sPref[b]);
+            if (b < B) pages_b = (sPref[b + 1] - sPref[b]) / Hkv;
+          }
+        }
+      }
+      if (lane == 0) {
+        if (!ok) {
+          *abort_flag = 1;
+          atomicOr(c.status, KVQ_STATUS_DEVICE_TIMEOUT);
+        }
+        // never leave while a copy may still be writing this CTA's shared memory (bounded)
+        for (int k = 1; k <= stages && k <= it; ++k) {
+          const int j = it - k;
+          mbar_wait(bar0 + 8 * (j % stages), (j / stages) & 1, wait_ns);
+        }
+      }
+      return;
+    }
+  }
+  if (!PAGED && KAXIS == 0 && warp == NW) {
     if (lane == 0) {
       int it = 0, stage = 0;
       uint32_t phase = 1;                // parity of the previous round of `empty`
@@ -713,7 +804,7 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
           for (int nh = 0; nh < NH; ++nh) {
             float q_all[NR][4];
             uint2 q_raw[NR];
-            load_q_raw<D>(g, q, b, h, (gid >> 1) + 4 * nh, tid, q_raw);
+            load_q_raw<D>(g, q, (size_t)b * g.rows, G, h, (gid >> 1) + 4 * nh, tid, q_raw);
             float am = convert_q_lane<D>(g, c, q_raw, tid, q_all);
 #pragma unroll
             for (int r = 0; r < HR; ++r) {
@@ -863,17 +954,26 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
 
   for (int x = x_lo; x < x_hi || (WIN && win_only);) {
     const int seg_pages = WIN && win_only ? 0 : min(pages_b - page, x_hi - x);
-    const int n_all = clamped_len(c.seq_len, b, g.capacity);
-    const int n_tok = g.R ? (n_all / g.R) * g.R : n_all;          // tokens of the sequence that are in the pages
+    const int n_all = PAGED ? sSeq[3 * b] : clamped_len(c.seq_len, b, g.capacity);
+    const int n_tok = !PAGED && g.R ? (n_all / g.R) * g.R : n_all;          // tokens of the sequence that are in the pages
+    const int rows = PAGED ? sSeq[3 * b + 1] : g.rows, G_seg = Gq * rows;          // query rows, (row, head) pairs per KV head
+    const size_t first_row = PAGED ? (size_t)sSeq[3 * b + 2] : (size_t)b * g.rows;
+    [[maybe_unused]] const SeenPages seen = seen_of(b);
+    // tokens that not every row sees: those from n_unmasked on and, with a window, those from `sinks` on in front of low_all (of
+    // which nobody sees those in front of low_any)
+    [[maybe_unused]] int low_all = 0, low_any = 0;
+    if constexpr (PAGED) {
+      if (pa.window > 0) { low_all = max(n_all - pa.window, 0); low_any = max(n_all - rows + 1 - pa.window, 0); }
+    }
     // a block is unmasked when all of its 32 tokens exist and every query row may see them (several causal rows:
     // row r sees the first n - (rows - 1 - r) tokens of the n the sequence holds, window included)
-    const int n_unmasked = min(n_tok, n_all - (g.rows - 1));
+    const int n_unmasked = min(n_tok, n_all - (rows - 1));
     const int stream = b * Hkv + h;
     // the queries are on their way while one warp works out
     [[maybe_unused]] uint2 q_raw[NH][NR];
     if constexpr (KAXIS == 0) {
 #pragma unroll
-      for (int nh = 0; nh < NH; ++nh) load_q_raw<D>(g, q, b, h, (gid >> 1) + 4 * nh, tid, q_raw[nh]);
+      for (int nh = 0; nh < NH; ++nh) load_q_raw<D>(g, q, first_row, G_seg, h, (gid >> 1) + 4 * nh, tid, q_raw[nh]);
     }
     // which of the stream's partials this CTA writes, and how many there are: one warp works it out now, everybody
     // reads it after the barrier at the segment's end (the barrier that closed the last segment keeps its readers apart)
@@ -969,15 +1069,23 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
 
     auto process = [&](auto full_tag, int pp) {
       constexpr bool FULL_PAGE = decltype(full_tag)::value;
-      const int nv = FULL_PAGE ? kPageTokens : min(kPageTokens, n_tok - (page + pp) * kPageTokens);
+      const int tok_page = PAGED ? seen.logical(page + pp) * kPageTokens : (page + pp) * kPageTokens;       // the page's first token
+      const int nv = FULL_PAGE ? kPageTokens : min(kPageTokens, n_tok - tok_page);
+      // whether some row sees tokens of a block of 32
+      auto block_on = [&](int blk) {
+        if (FULL_PAGE) return true;
+        if (PAGED && tok_page + 32 * blk + 32 <= low_any && tok_page + 32 * blk >= pa_sinks) return false;
+        return blk * 32 < nv;
+      };
       const bool tail_k = (KAXIS == 1) && (nv < kPageTokens);
       const uint8_t* sp = smem + stage * sl.page_stride;
       uint8_t* wbuf = smem + sl.w_off + (page_no & 1) * (NGV * 4 * WB);
       // ---- logits of the warp's 32 tokens, two tiles of 16; (scale, zero) of their values
       f32x2 L[2][NH];                    // [tile][head], of rows gid and gid + 8
       f32x2 sv[2][NGV], zv[2][NGV];
-      const bool active = FULL_PAGE || warp * 32 < nv;
-      const bool masked = !FULL_PAGE && (page + pp) * kPageTokens + warp * 32 + 32 > n_unmasked;
+      const bool active = block_on(warp);
+      const bool masked = !FULL_PAGE && (tok_page + warp * 32 + 32 > n_unmasked ||
+                                         (PAGED && tok_page + warp * 32 < low_all && tok_page + warp * 32 + 32 > pa_sinks));
       bool trig = false;
       float bmax[NH], smax = 0.f;
 #pragma unroll
@@ -1101,15 +1209,20 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
             zv[u][j] = pack2(fa.y, fb.y);
           }
           if (masked) {
-            const int tokg = (page + pp) * kPageTokens + tok0;        // position of row tok0 in the sequence
+            const int tokg = tok_page + tok0;        // position of row tok0 in the sequence
             const bool there0 = tok0 < nv, there1 = tok0 + 8 < nv;
 #pragma unroll
             for (int nh = 0; nh < NH; ++nh) {
               // tokens the lane's head may attend to: the causal limit of its query row
-              const int lim = n_all - (g.rows - 1 - min((tid + 4 * nh) / Gq, g.rows - 1));
+              const int lim = n_all - (rows - 1 - min((tid + 4 * nh) / Gq, rows - 1));
               float2 x = unpack2(L[u][nh]);
               if (!there0 || tokg >= lim) x.x = -INFINITY;
               if (!there1 || tokg + 8 >= lim) x.y = -INFINITY;
+              if constexpr (PAGED) {
+                const int low = pa.window > 0 ? lim - pa.window : 0;
+                if (tokg < low && tokg >= pa_sinks) x.x = -INFINITY;
+                if (tokg + 8 < low && tokg + 8 >= pa_sinks) x.y = -INFINITY;
+              }
               L[u][nh] = pack2(x.x, x.y);
             }
 #pragma unroll
@@ -1249,7 +1362,7 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
       // byte belongs to m-tile FPBV q + f, whose accumulators carry the factor 2^(VB f).
 #pragma unroll
       for (int blk = 0; blk < 4; ++blk) {
-        if (FULL_PAGE || blk * 32 < nv) {
+        if (block_on(blk)) {
           const uint8_t* w = wbuf + (jw * 4 + blk) * WB;
           uint32_t bw[NTV][2];
 #pragma unroll
@@ -1284,7 +1397,9 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
         if (!__all_sync(FULL, mbar_try_wait(bar0 + 8 * (2 * stages + stage), phase))) wait_slowly(bar0 + 8 * (2 * stages + stage));
       }
       // a page whose tokens all exist and may be seen by every query row needs no masks
-      if ((page + pp + 1) * kPageTokens <= n_unmasked) process(std::true_type{}, pp);
+      const int tok_page = PAGED ? seen.logical(page + pp) * kPageTokens : (page + pp) * kPageTokens;
+      const bool below = PAGED && tok_page < low_all && tok_page + kPageTokens > pa_sinks;       // the window ends inside the page
+      if (tok_page + kPageTokens <= n_unmasked && !below) process(std::true_type{}, pp);
       else process(std::false_type{}, pp);
       __syncwarp();
       mbar_arrive_if(bar0 + 8 * (stages + stage), lane == 0);
@@ -1323,7 +1438,7 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
 #pragma unroll
         for (int nh = 0; nh < NH; ++nh) {
           const int head = tid + 4 * nh;
-          if (head < G && !(WIN && win_only)) {
+          if (head < G_seg && !(WIN && win_only)) {
             float lsum = 0.f;
             double zsum = 0.0;
 #pragma unroll
@@ -1331,7 +1446,7 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
               lsum += sSum[w * 8 + head];
               zsum += sZ[(w * 8 + head) * NGV + jw];
             }
-            const size_t oi = (((size_t)b * g.rows + head / Gq) * g.Hq + (size_t)h * Gq + head % Gq) * D;
+            const size_t oi = ((first_row + head / Gq) * g.Hq + (size_t)h * Gq + head % Gq) * D;
             float* dst = ws + (((size_t)stream * s_cap + slot) * G + head) * (D + 2);
             if (!direct && warp == 0 && gid == 0) { dst[0] = m_ref[nh]; dst[1] = lsum; }
 #pragma unroll
@@ -1362,7 +1477,7 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
             // a warp per head, two or four channels per lane; eight partials' loads are in flight at a time
             constexpr int C2 = D / 64;
 #pragma unroll 1
-            for (int head = warp; head < G; head += NW) {
+            for (int head = warp; head < G_seg; head += NW) {
               const float* base = ws + (((size_t)stream * s_cap) * G + head) * (D + 2);
               const size_t slot_stride = (size_t)G * (D + 2);
               float mstar = -INFINITY, den = 0.f;
@@ -1399,7 +1514,7 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
                 }
                 mstar = mb;
               }
-              const size_t oi = (((size_t)b * g.rows + head / Gq) * g.Hq + (size_t)h * Gq + head % Gq) * D;
+              const size_t oi = ((first_row + head / Gq) * g.Hq + (size_t)h * Gq + head % Gq) * D;
 #pragma unroll
               for (int e = 0; e < C2; ++e) {
                 const float rx = den > 0.f ? num[e].x / den : 0.f, ry = den > 0.f ? num[e].y / den : 0.f;
@@ -1449,7 +1564,25 @@ int launch_mma_inst(const Geom& g, const CachePtrs& c, const void* q, float c1, 
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, sl.total) != cudaSuccess)
     return KVQ_ERR_CUDA_LAUNCH;
   const cudaError_t e = launch_dependent(kern, dim3(148 * MINB), (kConsumerWarps + 1) * 32, sl.total, stream, 1, g, c,
-                                         static_cast<const uint16_t*>(q), c1, ws, s_cap, stages, out, out_dtype, call_id, wait_ns, skip_x);
+                                         static_cast<const uint16_t*>(q), c1, ws, s_cap, stages, out, out_dtype, call_id, wait_ns, skip_x, NotPaged{});
+  return e == cudaSuccess ? KVQ_OK : KVQ_ERR_CUDA_LAUNCH;
+}
+
+// The same on a paged cache (its instantiations are in kvq_paged_decode_inst_*.cu).
+template <int D, int KB, int VB, int NGK, int NGV, int NH, int MINB>
+int launch_paged_inst(const Geom& g, const Paged& p, const void* q, float c1, float* ws, int s_cap, void* out, int out_dtype,
+                      unsigned long long call_id, unsigned long long wait_ns, long long skip_x, cudaStream_t stream) {
+  const int stages = ring_stages(g, NH, NGV, false, MINB, 5);
+  if (stages < 2) return KVQ_ERR_UNSUPPORTED;
+  const SmemLayout sl = smem_layout(g.page_bytes, stages, g.B, D, NH, NGV, false, 5);
+  auto kern = decode_mma_kernel<D, KB, VB, 0, NGK, NGV, NH, MINB, false, true>;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, sl.total) != cudaSuccess)
+    return KVQ_ERR_CUDA_LAUNCH;
+  CachePtrs c{};
+  c.pages = p.pages;
+  c.status = p.status;
+  const cudaError_t e = launch_dependent(kern, dim3(148 * MINB), (kConsumerWarps + 1) * 32, sl.total, stream, 1, g, c,
+                                         static_cast<const uint16_t*>(q), c1, ws, s_cap, stages, out, out_dtype, call_id, wait_ns, skip_x, p);
   return e == cudaSuccess ? KVQ_OK : KVQ_ERR_CUDA_LAUNCH;
 }
 

@@ -68,6 +68,10 @@ __host__ __device__ __forceinline__ SeenPages seen_pages(int p0, int p1, int win
 int launch_paged_append(const Geom& g, const Paged& p, const void* k, const void* v, int64_t kv_row, int64_t kv_head,
                         const RopeArgs& rope, const void* q, int64_t q_row, int64_t q_head, void* q_out, cudaStream_t stream);
 int launch_paged_dequantize(const Geom& g, const Paged& p, void* k_out, void* v_out, cudaStream_t stream);
+// up to eight (row, head) pairs per KV head (g.rows: the most rows of a sequence)
+bool paged_decode_supported(const Geom& g);
+int launch_paged_decode(const Geom& g, const Paged& p, const void* q, void* out, int out_dtype, float scale_log2e, float* ws,
+                        const DecodeDebug& dbg, cudaStream_t stream);
 int launch_paged_plain(const Geom& g, const Paged& p, const void* q, void* out, int out_dtype, float scale_log2e, cudaStream_t stream);
 
 }  // namespace kvq

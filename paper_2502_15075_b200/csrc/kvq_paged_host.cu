@@ -73,7 +73,8 @@ int kvq_paged_workspace_bytes(const kvq_config* cfg, int32_t max_rows, size_t* o
   const int rc = paged_geom(cfg, &g);
   if (rc != KVQ_OK) return rc;
   if (!out || max_rows < 1) return KVQ_ERR_INVALID_ARG;
-  *out = 16;
+  g.rows = max_rows;
+  *out = paged_decode_supported(g) ? flat_workspace_bytes(g) : 16;
   return KVQ_OK;
 }
 
@@ -94,11 +95,15 @@ int kvq_paged_attention(const kvq_config* cfg, const kvq_paged_cache* cache, con
   rc = kvq_paged_workspace_bytes(cfg, max_rows, &need);
   if (rc != KVQ_OK) return rc;
   if (workspace_bytes < need) return KVQ_ERR_WORKSPACE_TOO_SMALL;
+  g.rows = max_rows;
   p.max_rows = max_rows;
   p.window = window;
   p.sinks = sinks;
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)g.D);
-  return launch_paged_plain(g, p, q, out, out_dtype, scale * 1.4426950408889634f, static_cast<cudaStream_t>(cuda_stream));
+  const float c1 = scale * 1.4426950408889634f;
+  const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  if (paged_decode_supported(g)) return launch_paged_decode(g, p, q, out, out_dtype, c1, static_cast<float*>(workspace), DecodeDebug{}, stream);
+  return launch_paged_plain(g, p, q, out, out_dtype, c1, stream);
 }
 
 int kvq_paged_dequantize(const kvq_config* cfg, const kvq_paged_cache* cache, const int32_t* cu, int32_t n_rows, void* k_out,
