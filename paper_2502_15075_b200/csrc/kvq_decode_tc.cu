@@ -27,7 +27,7 @@
 
 #include <mutex>
 
-#include "kvq_decode_mma.cuh"
+#include "kvq_tcgen05.cuh"
 
 namespace kvq {
 namespace tc {
@@ -74,23 +74,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;"
       ::"r"(dst), "l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "l"(policy) : "memory");
 }
-__device__ __forceinline__ void tmem_alloc(uint32_t dst_smem, uint32_t ncols) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(ncols) : "memory");
-}
-__device__ __forceinline__ void tmem_relinquish() {
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {
-  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
 // D[tmem] (+)= A[tmem] * B[smem descriptor], 8-bit integer operands, int32 accumulate.
 __device__ __forceinline__ void tc_mma_i8_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
                                              uint32_t accumulate) {
@@ -130,28 +113,10 @@ __device__ __forceinline__ bool cons_bar_or(bool pred) {
   return r != 0;
 }
 
-// Shared-memory matrix descriptors (no swizzle, version 1): start address, leading (K-direction) and stride
-// (M/N-direction) byte offsets of the 8 x 16-byte core matrices, all in units of 16 bytes.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
-  return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)((lbo_bytes >> 4) & 0x3FFF) << 16) |
-         ((uint64_t)((sbo_bytes >> 4) & 0x3FFF) << 32) | (1ull << 46);
-}
 // Instruction descriptors: int32 accumulate, A unsigned bytes (K-major, from tensor memory), M 128, N 16;
 // QK^T: B signed bytes K-major; PV: B unsigned bytes N-major.
 constexpr uint32_t kIdescQK = (2u << 4) | (0u << 7) | (1u << 10) | (0u << 16) | (2u << 17) | (8u << 24);
 constexpr uint32_t kIdescPV = (2u << 4) | (0u << 7) | (0u << 10) | (1u << 16) | (2u << 17) | (8u << 24);
-
-// Wait that also gives up early when another role of the CTA has already given up.
-__device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, unsigned long long limit_ns,
-                                              volatile int* abort_flag) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const unsigned long long t0 = globaltimer_ns();
-  while (true) {
-    if (mbar_try_wait_hint(bar, parity, 2000u)) return true;
-    if (*abort_flag) return false;
-    if (globaltimer_ns() - t0 > limit_ns) return false;
-  }
-}
 
 template <int KB, int VB, int MINB>
 __global__ void __launch_bounds__(kThreads, MINB)

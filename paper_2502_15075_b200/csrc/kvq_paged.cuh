@@ -72,6 +72,9 @@ int launch_paged_dequantize(const Geom& g, const Paged& p, void* k_out, void* v_
 bool paged_decode_supported(const Geom& g);
 int launch_paged_decode(const Geom& g, const Paged& p, const void* q, void* out, int out_dtype, float scale_log2e, float* ws,
                         const DecodeDebug& dbg, cudaStream_t stream);
-int launch_paged_plain(const Geom& g, const Paged& p, const void* q, void* out, int out_dtype, float scale_log2e, cudaStream_t stream);
+// any number of rows
+size_t paged_chunk_workspace_bytes(const Geom& g);
+int launch_paged_chunk(const Geom& g, const Paged& p, const void* q, void* out, int out_dtype, float scale_log2e, float* ws,
+                       const DecodeDebug& dbg, cudaStream_t stream);
 
 }  // namespace kvq

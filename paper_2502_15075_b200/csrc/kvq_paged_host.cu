@@ -1,6 +1,7 @@
 // C-ABI of the paged cache: argument checks and dispatch.
 #include <math.h>
 
+#include "kvq_debug.h"
 #include "kvq_paged.cuh"
 
 using namespace kvq;
@@ -33,6 +34,34 @@ int paged_args(const Geom& g, const kvq_paged_cache* c, const int32_t* cu, int32
 int rows_ok(const Geom& g, const void* x, int64_t row, int64_t head, int heads, int n_rows) {
   if ((n_rows > 1 && row < g.D) || (heads > 1 && head < g.D)) return KVQ_ERR_INVALID_ARG;
   return !aligned16(x) || (n_rows > 1 && row % 8) || (heads > 1 && head % 8) ? KVQ_ERR_MISALIGNED : KVQ_OK;
+}
+
+int attention_with(const DecodeDebug& dbg, const kvq_config* cfg, const kvq_paged_cache* cache, const void* q, const int32_t* cu, int32_t n_rows,
+                   int32_t max_rows, int32_t window, int32_t sinks, void* out, int32_t out_dtype, float softmax_scale,
+                   void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  Geom g;
+  Paged p;
+  int rc = paged_geom(cfg, &g);
+  if (rc == KVQ_OK) rc = paged_args(g, cache, cu, n_rows, &p);
+  if (rc != KVQ_OK) return rc;
+  if (max_rows < 1 || window < 0 || sinks < 0) return KVQ_ERR_INVALID_ARG;
+  if (n_rows == 0) return KVQ_OK;
+  if (!q || !out || !workspace) return KVQ_ERR_INVALID_ARG;
+  if (out_dtype != KVQ_FP16 && out_dtype != KVQ_BF16 && out_dtype != KVQ_FP32) return KVQ_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return KVQ_ERR_MISALIGNED;
+  size_t need = 0;
+  rc = kvq_paged_workspace_bytes(cfg, max_rows, &need);
+  if (rc != KVQ_OK) return rc;
+  if (workspace_bytes < need) return KVQ_ERR_WORKSPACE_TOO_SMALL;
+  g.rows = max_rows;
+  p.max_rows = max_rows;
+  p.window = window;
+  p.sinks = sinks;
+  const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)g.D);
+  const float c1 = scale * 1.4426950408889634f;
+  const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  auto launch = paged_decode_supported(g) ? launch_paged_decode : launch_paged_chunk;
+  return launch(g, p, q, out, out_dtype, c1, static_cast<float*>(workspace), dbg, stream);
 }
 
 }  // namespace
@@ -74,36 +103,26 @@ int kvq_paged_workspace_bytes(const kvq_config* cfg, int32_t max_rows, size_t* o
   if (rc != KVQ_OK) return rc;
   if (!out || max_rows < 1) return KVQ_ERR_INVALID_ARG;
   g.rows = max_rows;
-  *out = paged_decode_supported(g) ? flat_workspace_bytes(g) : 16;
+  *out = paged_decode_supported(g) ? flat_workspace_bytes(g) : paged_chunk_workspace_bytes(g);
   return KVQ_OK;
 }
 
 int kvq_paged_attention(const kvq_config* cfg, const kvq_paged_cache* cache, const void* q, const int32_t* cu, int32_t n_rows,
                         int32_t max_rows, int32_t window, int32_t sinks, void* out, int32_t out_dtype, float softmax_scale,
                         void* workspace, size_t workspace_bytes, void* cuda_stream) {
-  Geom g;
-  Paged p;
-  int rc = paged_geom(cfg, &g);
-  if (rc == KVQ_OK) rc = paged_args(g, cache, cu, n_rows, &p);
-  if (rc != KVQ_OK) return rc;
-  if (max_rows < 1 || window < 0 || sinks < 0) return KVQ_ERR_INVALID_ARG;
-  if (n_rows == 0) return KVQ_OK;
-  if (!q || !out || !workspace) return KVQ_ERR_INVALID_ARG;
-  if (out_dtype != KVQ_FP16 && out_dtype != KVQ_BF16 && out_dtype != KVQ_FP32) return KVQ_ERR_INVALID_ARG;
-  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return KVQ_ERR_MISALIGNED;
-  size_t need = 0;
-  rc = kvq_paged_workspace_bytes(cfg, max_rows, &need);
-  if (rc != KVQ_OK) return rc;
-  if (workspace_bytes < need) return KVQ_ERR_WORKSPACE_TOO_SMALL;
-  g.rows = max_rows;
-  p.max_rows = max_rows;
-  p.window = window;
-  p.sinks = sinks;
-  const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)g.D);
-  const float c1 = scale * 1.4426950408889634f;
-  const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  if (paged_decode_supported(g)) return launch_paged_decode(g, p, q, out, out_dtype, c1, static_cast<float*>(workspace), DecodeDebug{}, stream);
-  return launch_paged_plain(g, p, q, out, out_dtype, c1, stream);
+  return attention_with(DecodeDebug{}, cfg, cache, q, cu, n_rows, max_rows, window, sinks, out, out_dtype, softmax_scale, workspace,
+                        workspace_bytes, cuda_stream);
+}
+
+int kvq_debug_paged_stall(const kvq_config* cfg, const kvq_paged_cache* cache, const void* q, const int32_t* cu, int32_t n_rows,
+                          int32_t max_rows, int32_t window, int32_t sinks, void* out, int32_t out_dtype, void* workspace,
+                          size_t workspace_bytes, int64_t skip_page, uint32_t wait_us, void* cuda_stream) {
+  if (wait_us == 0 || wait_us > 100000u) return KVQ_ERR_INVALID_ARG;      // the hook never waits longer than 0.1 s
+  DecodeDebug dbg;
+  dbg.skip_page = skip_page;
+  dbg.wait_us = wait_us;
+  return attention_with(dbg, cfg, cache, q, cu, n_rows, max_rows, window, sinks, out, out_dtype, 0.0f, workspace, workspace_bytes,
+                        cuda_stream);
 }
 
 int kvq_paged_dequantize(const kvq_config* cfg, const kvq_paged_cache* cache, const int32_t* cu, int32_t n_rows, void* k_out,

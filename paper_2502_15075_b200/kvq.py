@@ -93,6 +93,8 @@ _lib.kvq_paged_attention.argtypes = [_P(kvq_config), _P(kvq_paged_cache), ctypes
     ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
 _lib.kvq_paged_dequantize.argtypes = [_P(kvq_config), _P(kvq_paged_cache), ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
                                       ctypes.c_void_p, ctypes.c_void_p]
+_lib.kvq_debug_paged_stall.argtypes = [_P(kvq_config), _P(kvq_paged_cache), ctypes.c_void_p, ctypes.c_void_p] + [ctypes.c_int32] * 4 + [
+    ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64, ctypes.c_uint32, ctypes.c_void_p]
 _lib.kvq_paged_check_status.argtypes = [_P(kvq_paged_cache), ctypes.c_void_p]
 _lib.kvq_check_status.argtypes = [_P(kvq_cache), ctypes.c_void_p]
 _lib.kvq_strerror.argtypes = [ctypes.c_int]
@@ -102,7 +104,7 @@ for _f in ("kvq_page_bytes", "kvq_cache_bytes", "kvq_workspace_bytes", "kvq_quan
            "kvq_quant_error", "kvq_bit_balance", "kvq_debug_decode_generic", "kvq_debug_decode_stall",
            "kvq_debug_decode_impl", "kvq_debug_decode_stall_impl", "kvq_debug_decode_plan", "kvq_debug_decode_ring", "kvq_debug_decode_windows",
            "kvq_debug_divide", "kvq_workspace_bytes_rows", "kvq_decode_attention_rows", "kvq_paged_append", "kvq_paged_workspace_bytes",
-           "kvq_paged_attention", "kvq_paged_dequantize", "kvq_paged_check_status"):
+           "kvq_paged_attention", "kvq_paged_dequantize", "kvq_paged_check_status", "kvq_debug_paged_stall"):
     getattr(_lib, _f).restype = ctypes.c_int
 
 EXPORTS = ("kvq_layout_version", "kvq_page_bytes", "kvq_cache_bytes", "kvq_workspace_bytes",
@@ -510,6 +512,15 @@ def kvq_paged_attention(cfg: kvq_config, cache: PagedCache, q: torch.Tensor, cu:
                                     int(window), int(sinks), out.data_ptr(), _dtype_code(out.dtype), float(softmax_scale),
                                     workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
            "kvq_paged_attention")
+
+
+def kvq_debug_paged_stall(cfg: kvq_config, cache: PagedCache, q: torch.Tensor, cu: torch.Tensor, out: torch.Tensor,
+                          workspace: torch.Tensor, max_rows: int, skip_page: int, wait_us: int):
+    """Test hook: kvq_paged_attention with one page withheld and every device-side wait limited to wait_us."""
+    _check(_lib.kvq_debug_paged_stall(ctypes.byref(cfg), ctypes.byref(cache.c), q.data_ptr(), cu.data_ptr(), q.shape[0], int(max_rows), 0, 0,
+                                      out.data_ptr(), _dtype_code(out.dtype), workspace.data_ptr(),
+                                      workspace.numel() * workspace.element_size(), int(skip_page), int(wait_us), _stream_ptr(None)),
+           "kvq_debug_paged_stall")
 
 
 def kvq_paged_dequantize(cfg: kvq_config, cache: PagedCache, cu: torch.Tensor, k_out: Optional[torch.Tensor],

@@ -250,3 +250,17 @@ def test_prompt_chunks_and_decoding_in_turn(kvq):
         assert kvq.kvq_check_status(cache) == 0
         want = pt.attention(cache.pages.cpu().numpy(), sh, call.table, lens, cu.cpu().numpy(), q.double().cpu().numpy(), window, sinks, np.zeros(q.shape))
         close(out.double().cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("rows,skip", [(1, 0), (1, 3), (1, 9), (40, 0), (40, 5), (40, 11), (300, 7)])
+def test_a_page_that_never_arrives_ends_the_call(kvq, rows, skip):
+    """The bounded waits run out, the call ends with a status, and the next call on the same workspace is right."""
+    call = pt.Call(kvq, S(), [700, 500], [rows, 1], 0, 0, seed=15)
+    cache, cu = call.on_gpu()
+    q = call.q.cuda()
+    ws = torch.empty(kvq.kvq_paged_workspace_bytes(call.cfg, rows), dtype=torch.uint8, device="cuda")
+    out = torch.zeros(q.shape, device="cuda")
+    kvq.kvq_debug_paged_stall(call.cfg, cache, q, cu, out, ws, rows, skip, 2000)
+    assert kvq.kvq_check_status(cache) == -7
+    cache.status.zero_()
+    close(call.got_attention(cache=cache, cu=cu, workspace=ws), call.want_attention())
