@@ -46,6 +46,36 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int B, int i, int 
   return min(lo + __popc(__ballot_sync(0xffffffffu, passed)), B - 1);
 }
 
+// The rows of a call by aligned blocks of `span` tokens of their sequences (a power of two): block `slot` of at most block_tasks(...) of them.
+// Sequence b has the slots from cu[b] / span + 2 b on: r rows touch at most r / span + 2 blocks.
+struct BlockTask { int b, t0, lo, hi; long long row0; };      // tokens t0 + lo .. t0 + hi - 1 of sequence b are rows row0 + lo .. (lo >= hi: none)
+__host__ __device__ inline long long block_tasks(int n_rows, int B, int span) { return n_rows / span + 2ll * B; }
+__device__ __forceinline__ BlockTask block_task(const Paged& p, int B, int slot, int span, int limit, int max_rows, int lane) {
+  int lo = 0, len = B;                           // the last sequence whose slots start at or below this one, in pieces as in sequence_of
+  while (len > 1) {
+    const int step = (len + 31) >> 5, at = lo + lane * step;
+    const bool below = at < lo + len && p.cu[at] / span + 2 * at <= slot;
+    const int k = __popc(__ballot_sync(0xffffffffu, below));
+    const int piece = k > 0 ? k - 1 : 0, end = lo + len;
+    lo += piece * step;
+    len = min(step, end - lo);
+  }
+  bool bad;
+  const SeqRows s = seq_rows(p, lo, limit, max_rows, bad);
+  if (bad && lane == 0) atomicOr(p.status, KVQ_STATUS_BAD_INPUT);
+  BlockTask t{lo, 0, 0, 0, 0};
+  if (s.rows == 0) return t;
+  const int start = s.n - s.rows, skipped = slot - (s.first / span + 2 * lo);
+  if (skipped < 0) return t;
+  const long long t0 = (long long)(start / span) * span + (long long)skipped * span;
+  if (t0 >= s.n) return t;
+  t.t0 = (int)t0;
+  t.lo = max(start - t.t0, 0);
+  t.hi = min(s.n - t.t0, span);
+  t.row0 = (long long)s.first - start + t.t0;
+  return t;
+}
+
 // Pool page of logical page `page` of sequence b, or -1 (outside the pool).
 __device__ __forceinline__ int pool_page(const Paged& p, int b, int page) {
   const int id = p.table[(long long)b * p.table_stride + page];

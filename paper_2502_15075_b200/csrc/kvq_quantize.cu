@@ -35,224 +35,6 @@ struct RowSrc {
   }
 };
 
-// Tokens handled by one warp task: 32, or 64 where 32 tokens would leave a lane fewer than the four tokens
-// that make up a word of value codes.
-__host__ __device__ constexpr int task_tokens(int D, int bits) { return (D == 64 && bits == 2) ? 64 : 32; }
-
-// Value e (0..7) of a 16-byte piece in fp32.
-template <int DTYPE>
-__device__ __forceinline__ float piece_value(const uint4& r, int e) {
-  const uint32_t w = e < 2 ? r.x : e < 4 ? r.y : e < 6 ? r.z : r.w;
-  if constexpr (DTYPE == KVQ_BF16) return __uint_as_float((e & 1) ? (w & 0xFFFF0000u) : (w << 16));
-  else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w)); return (e & 1) ? f.y : f.x; }
-}
-
-// Task-local token of token slot k: of the four of a value word (slots 4 i .. 4 i + 3), or of a key row.
-template <bool IS_V, int RS>
-__device__ __forceinline__ int token_slot(int k, int rs) {
-  if constexpr (IS_V) {
-    const int cmb = (k >> 2) * RS + rs, j = k & 3;         // cmb = (block, half, t) of the word; j = byte
-    return 32 * (cmb >> 3) + 16 * ((cmb >> 2) & 1) + 2 * (cmb & 3) + (j >> 1) + 8 * (j & 1);
-  } else {
-    return k * RS + rs;
-  }
-}
-
-// Tokens of a lane per pass: four make up a word of value codes.  Keys at 2 bits, whose pieces of four tokens would take 64 registers
-// beside those of the arithmetic, go by two and in passes of 4 KB, as most sides do: four layers of 40 streams x 3,000 tokens K2V4 92 us by
-// four, 87.5 by two; two of 64 x 4,000 81.7 and 78.8.
-__host__ __device__ constexpr int pass_tokens(int bits, bool is_v) { return bits == 2 && !is_v ? 2 : 4; }
-
-// One pass over pass_tokens tokens of every lane, one side of a task of TT tokens; tokens [lo, hi) of the task are new.  load(kk, f): the
-// lane's piece f of its token kk.  next is called when the pieces have been read.  codes: keys - the page's key row of the task's first
-// token; values - the page's value block of the task's first token.  meta_out: metadata row of the task's first token.
-//
-// Lane = (row slot rs, word column mw, row half rh): it owns, for each of its tokens, the FPB pieces of 8 channels
-// 16 (FPB mw + f) + 8 rh + {0..7}, f < FPB, whose codes share bytes.  The minima / maxima of its tokens are reduced
-// with a shuffle reduce-scatter, so that the group parameters (two divisions) are computed once per group rather than once
-// per lane, and are then broadcast to the lanes of the group.  Minimum and negated maximum travel as one pair of the 16-bit type.
-// PLAIN: if all groups of the warp are plain (see plain_group; all but those with values beyond the fp16 range or scales and minima
-// below its normal numbers are), codes need no clamp and two values share every operation: 8.7 instructions per element instead of
-// 10.6; else nothing is stored and the answer is false.  A value word's two ways of leaving, whole or byte by byte, are one branch behind
-// all eight words (a branch per word: 8 streams x 500 tokens K4V2 11.8 us against 8.7).
-template <int BITS, bool IS_V, int D, int DTYPE, bool PLAIN, typename Load, typename Next>
-__device__ __forceinline__ bool quantize_pass(Load&& load, Next&& next, int gsz, int lo, int hi, uint8_t* __restrict__ codes,
-                                              uint32_t* __restrict__ meta_out, int lane, int pass) {
-  using H2 = typename Pair16<DTYPE>::type;
-  constexpr int FPB = 8 / BITS, TK = pass_tokens(BITS, IS_V);
-  constexpr int NMW = (D / 16) / FPB;        // word columns per row half
-  constexpr int LR = 2 * NMW;                // lanes per token row
-  constexpr int RS = 32 / LR;                // token rows per load instruction
-  constexpr int K_ROW_BYTES = D * BITS / 8;
-  constexpr int NSET = FPB == 4 ? 2 : 1;      // a lane's fields may belong to two groups (groups of 32 at 2 bits)
-  constexpr float DOWN = 1.0f / (float)(1 << BITS);
-  const int rs = lane / LR, cs = lane % LR, mw = cs >> 1, rh = cs & 1;
-  const float qmax = (float)((1 << BITS) - 1);
-  const int spg = gsz >> 4;                                  // 16-channel slices per group
-  const bool split = FPB > spg;
-  const int lpg = split ? 2 : 2 * spg / FPB;                 // lanes per group: 2, 4, 8 or 16
-  const int ng = D / gsz;
-  const int b0 = cs & 1, b1 = (cs >> 1) & 1;
-  const int gbase = lane & ~(lpg - 1);                       // first lane of this lane's group
-
-  auto token_of = [&](int k) { return token_slot<IS_V, RS>(k, rs); };
-  auto swap = [](H2 x, int off) {
-    const uint32_t o = __shfl_xor_sync(FULL, *reinterpret_cast<uint32_t*>(&x), off);
-    return *reinterpret_cast<const H2*>(&o);
-  };
-
-  uint4 raw[TK][FPB];
-  bool valid[TK];
-#pragma unroll
-  for (int kk = 0; kk < TK; ++kk) {
-    const int tau = token_of(TK * pass + kk);
-    valid[kk] = tau >= lo && tau < hi;
-#pragma unroll
-    for (int f = 0; f < FPB; ++f) raw[kk][f] = load(kk, f);
-  }
-  // ---- minima / maxima of the lane's fields, per token and per set
-  H2 m[NSET][TK];
-#pragma unroll
-  for (int kk = 0; kk < TK; ++kk) {
-    m[0][kk] = minmax8<DTYPE, PLAIN>(raw[kk][0]);
-    if constexpr (FPB == 2) m[0][kk] = min_pair(m[0][kk], minmax8<DTYPE, PLAIN>(raw[kk][1]), PLAIN);
-    if constexpr (FPB == 4) {
-      m[0][kk] = min_pair(m[0][kk], minmax8<DTYPE, PLAIN>(raw[kk][1]), PLAIN);
-      m[1][kk] = min_pair(minmax8<DTYPE, PLAIN>(raw[kk][2]), minmax8<DTYPE, PLAIN>(raw[kk][3]), PLAIN);
-      if (!split) m[0][kk] = min_pair(m[0][kk], m[1][kk], PLAIN);
-    }
-  }
-  // ---- reduce-scatter over the lanes of the group: after lane bit 0 a lane holds tokens 2 b0 + {0, 1}, after
-  // bit 1 (groups of 4 lanes or more) token 2 b0 + b1; of two tokens it holds token b0; higher bits are plain butterflies
-  float pz[NSET][2], pinv[NSET][2];
-  uint32_t pmeta[NSET][2];
-  bool plain = true;
-#pragma unroll
-  for (int e = 0; e < NSET; ++e) {
-    if (e == 1 && !split) break;
-    H2 a0, a1;
-    if constexpr (TK == 4) {
-      a0 = min_pair(b0 ? m[e][2] : m[e][0], swap(b0 ? m[e][0] : m[e][2], 1), PLAIN);
-      a1 = min_pair(b0 ? m[e][3] : m[e][1], swap(b0 ? m[e][1] : m[e][3], 1), PLAIN);
-      if (lpg >= 4) a0 = min_pair(b1 ? a1 : a0, swap(b1 ? a0 : a1, 2), PLAIN);
-    } else {
-      a0 = a1 = min_pair(b0 ? m[e][1] : m[e][0], swap(b0 ? m[e][0] : m[e][1], 1), PLAIN);
-      if (lpg >= 4) a0 = min_pair(a0, swap(a0, 2), PLAIN);
-    }
-    if (lpg >= 8) a0 = min_pair(a0, swap(a0, 4), PLAIN);
-    if (lpg >= 16) a0 = min_pair(a0, swap(a0, 8), PLAIN);
-    const float2 f0 = pair_to_f32(a0);
-    const GroupParams p0 = group_params(f0.x, -f0.y, qmax);
-    if constexpr (PLAIN) plain &= plain_group(f0.x, -f0.y, p0, qmax);
-    pz[e][0] = p0.z; pinv[e][0] = p0.inv * DOWN; pmeta[e][0] = p0.meta;
-    pz[e][1] = 0.f; pinv[e][1] = 0.f; pmeta[e][1] = 0u;
-    if (TK == 4 && lpg == 2) {
-      const float2 f1 = pair_to_f32(a1);
-      const GroupParams p1 = group_params(f1.x, -f1.y, qmax);
-      if constexpr (PLAIN) plain &= plain_group(f1.x, -f1.y, p1, qmax);
-      pz[e][1] = p1.z; pinv[e][1] = p1.inv * DOWN; pmeta[e][1] = p1.meta;
-    }
-  }
-  next();                                   // (the shuffles above have seen all of `raw`: its place may be filled again)
-  if constexpr (PLAIN) {
-    if (!__all_sync(FULL, plain)) return false;
-  }
-  // the lane (one per group) that holds a token's parameters stores its metadata word
-  if ((cs & (lpg - 1) & -TK) == 0) {
-#pragma unroll
-    for (int e = 0; e < NSET; ++e) {
-      if (e == 1 && !split) break;
-      const int gi = (16 * FPB * mw) / gsz + e;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (i == 1 && (TK == 2 || lpg != 2)) break;
-        const int kk = TK == 2 ? b0 : 2 * b0 + (lpg >= 4 ? b1 : i);
-        const int tau = token_of(TK * pass + kk);
-        if (tau >= lo && tau < hi) meta_out[tau * ng + gi] = pmeta[e][i];
-      }
-    }
-  }
-  // ---- the group's parameters, fetched from the lane that made them
-  float z[NSET][TK], inv[NSET][TK];
-#pragma unroll
-  for (int kk = 0; kk < TK; ++kk) {
-    const int srcl = gbase + (TK == 2 ? kk : lpg >= 4 ? (kk >> 1) + 2 * (kk & 1) : (kk >> 1));
-    const int el = TK == 2 || lpg >= 4 ? 0 : kk & 1;
-    z[0][kk] = __shfl_sync(FULL, el ? pz[0][1] : pz[0][0], srcl);
-    inv[0][kk] = __shfl_sync(FULL, el ? pinv[0][1] : pinv[0][0], srcl);
-    if constexpr (NSET == 2) {
-      z[1][kk] = z[0][kk]; inv[1][kk] = inv[0][kk];
-      if (split) {
-        z[1][kk] = __shfl_sync(FULL, el ? pz[1][1] : pz[1][0], srcl);
-        inv[1][kk] = __shfl_sync(FULL, el ? pinv[1][1] : pinv[1][0], srcl);
-      }
-    }
-  }
-  if constexpr (!IS_V) {
-    // ---- keys: the four bytes of a word are channels 4 hh + {0..3} of this lane's 8, chunk 2 rh + hh, word mw of the row
-    constexpr int wpc = D * BITS / 128;
-#pragma unroll
-    for (int kk = 0; kk < TK; ++kk) {
-      const int tau = token_of(TK * pass + kk);
-#pragma unroll
-      for (int hh = 0; hh < 2; ++hh) {
-        uint32_t w = 0;
-#pragma unroll
-        for (int f = FPB - 1; f >= 0; --f) {
-          const int e = NSET == 2 ? f >> 1 : 0;
-          float x[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] = piece_value<DTYPE>(raw[kk][f], 4 * hh + j);
-          if constexpr (PLAIN) {
-            const f32x2 nz = pack2(-z[e][kk], -z[e][kk]), ii = pack2(inv[e][kk], inv[e][kk]);
-            w = w * (1u << BITS) + code_word4_plain<BITS>(pack2(x[0], x[1]), pack2(x[2], x[3]), nz, nz, ii, ii);
-          } else {
-            const float zz[4] = {z[e][kk], z[e][kk], z[e][kk], z[e][kk]}, ii[4] = {inv[e][kk], inv[e][kk], inv[e][kk], inv[e][kk]};
-            w = w * (1u << BITS) + code_word4<BITS>(x, zz, ii);
-          }
-        }
-        if (valid[kk])
-          *reinterpret_cast<uint32_t*>(codes + (size_t)tau * K_ROW_BYTES + chunk_word_byte(2 * rh + hh, mw, wpc, 4)) = w;
-      }
-    }
-  } else {
-    // ---- values: the four bytes of a word are this lane's four tokens; word of channel slot i at lane chunk 4 i + t
-    const int cmb = pass * RS + rs;
-    uint8_t* wbase = codes + (size_t)(cmb >> 3) * (4 * D * BITS) + mw * 512 + (cmb & 3) * 16 +
-                     4 * (2 * rh + ((cmb >> 2) & 1));
-    uint32_t w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      w[i] = 0;
-#pragma unroll
-      for (int f = FPB - 1; f >= 0; --f) {
-        const int e = NSET == 2 ? f >> 1 : 0;
-        float x[4];
-#pragma unroll
-        for (int kk = 0; kk < TK; ++kk) x[kk] = piece_value<DTYPE>(raw[kk][f], i);
-        if constexpr (PLAIN)
-          w[i] = w[i] * (1u << BITS) + code_word4_plain<BITS>(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(-z[e][0], -z[e][1]), pack2(-z[e][2], -z[e][3]),
-                                                        pack2(inv[e][0], inv[e][1]), pack2(inv[e][2], inv[e][3]));
-        else
-          w[i] = w[i] * (1u << BITS) + code_word4<BITS>(x, z[e], inv[e]);
-      }
-    }
-    if (valid[0] && valid[1] && valid[2] && valid[3]) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) *reinterpret_cast<uint32_t*>(wbase + 64 * i) = w[i];
-    } else {
-#pragma unroll
-      for (int kk = 0; kk < TK; ++kk) {
-        if (valid[kk]) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) wbase[64 * i + kk] = (uint8_t)(w[i] >> (8 * kk));
-        }
-      }
-    }
-  }
-  return true;
-}
-
 // The same with clamped codes, out of line: few passes need it.
 template <int BITS, bool IS_V, int D, int DTYPE>
 __device__ __noinline__ void quantize_pass_clamped(RowSrc rsrc, int gsz, int lo, int hi, uint8_t* __restrict__ codes,
