@@ -3,11 +3,11 @@
 //
 // A tile is 256 (query row, head) pairs of one sequence and KV head - the query heads of a KV head are rows of one product - against pages of 128
 // tokens.  One CTA per SM:
-//  * warps 8-11 turn a page into 16-bit tiles in shared memory: codes become fp16 by a byte permute and an exact subtraction, scale and
-//    zero-point enter by one fused operation (one rounding, 2^-11 of the value at most).  Their packed words were loaded a page ahead, straight
-//    into registers.  The order of channels (keys) and of tokens (both) is the one in which codes lie in the page; queries and the weights
-//    follow it, so that nothing is transposed.
-//  * one thread of warp 12 issues tcgen05.mma (kind f16, M 128, fp32 accumulators in tensor memory): S = Q K^T of both halves of the tile
+//  * warps 8-15 (keys) and 16-23 (values) turn a page into 16-bit tiles in shared memory: codes become fp16 by a mask under the bits of 1024 and
+//    an exact operation, scale and zero-point enter by a fused one (one rounding, 2^-11 of the value at most).  Their packed words were
+//    loaded a page ahead, straight into registers.  The order of channels (keys) and of tokens (both) is the one in which codes lie in the
+//    page; queries and the weights follow it, so that nothing is transposed.
+//  * one thread of warp 24 issues tcgen05.mma (kind f16, M 128, fp32 accumulators in tensor memory): S = Q K^T of both halves of the tile
 //    in turn, and O += P V with P read from tensor memory, where it takes the place of S.
 //  * warps 0-3 and 4-7 take the two halves, a thread per row: row maximum, p = 2^(x - reference), fp16 weights back to tensor memory;
 //    sums in fp32.  While one half's softmax runs, the tensor cores have the other half's products.  The reference moves only when a logit
@@ -29,11 +29,14 @@ namespace kvq {
 namespace chunk {
 
 using namespace mma;
-using tc::smem_desc;
 
-constexpr int kThreads = 13 * 32;
+constexpr int kThreads = 28 * 32;          // warps 0-7 softmax, 8-15 keys, 16-23 values, 24 products (25-27 complete its warpgroup)
+// Registers per thread at launch, and of the roles: 256 softmax threads, 512 that make tiles, 128 more.
+constexpr int kRegsLaunch = 72, kRegsSoftmax = 104, kRegsTiles = 56, kRegsRest = 72;
+static_assert(256 * kRegsSoftmax + 512 * kRegsTiles + 128 * kRegsRest <= kThreads * kRegsLaunch, "an increase waits for registers that the others gave up");
 constexpr int kGrid = 148;
 constexpr int kTile = 256;                 // (query row, head) pairs of a tile
+constexpr int kGap = 2;                    // what a tile costs besides its pages (queries, a first product that nothing overlaps, outputs), in pages
 constexpr float kHeadroom = 4.0f;
 constexpr float kBigDown = 9.765625e-4f, kBigUp = 1024.0f;      // 2^-10 for pages whose values pass half the fp16 range, and back
 constexpr uint32_t FULL = 0xffffffffu;
@@ -42,10 +45,10 @@ constexpr uint32_t kColS = 0, kColO = 256, kTmemCols = 512;
 // fp16 operands, fp32 accumulate, both K-major, M 128
 __host__ __device__ constexpr uint32_t idesc(int n) { return (1u << 4) | ((uint32_t)(n / 8) << 17) | (8u << 24); }
 
-// Shared memory.  Operands lie in 8 x 16-byte core matrices: rows 16 bytes apart, octets of rows 128, chunks of eight k `lb` apart (keys and
-// values 32 bytes more than dense, which spreads the writers' lanes over the banks).
+// Shared memory.  Operands lie in 8 x 16-byte core matrices: rows 16 bytes apart, octets of rows 128, chunks of eight k `lb` apart; eight
+// neighbouring lanes write one core matrix.
 template <int D> struct Tiles {
-  static constexpr int kLbQ = 128 * 16, kLbK = 128 * 16 + 32, kLbV = D * 16 + 32;
+  static constexpr int kLbQ = 128 * 16, kLbK = 128 * 16, kLbV = D * 16;
   static constexpr int kQ = D / 8 * kLbQ, kK = D / 8 * kLbK, kV = 16 * kLbV;      // bytes of a query half, a key and a value tile
 };
 struct Smem { int q, k, v, bars, misc, pref, seq, total; };
@@ -71,13 +74,25 @@ __host__ __device__ inline size_t count_offset_floats(int cap, int D) { return m
 __host__ __device__ inline size_t workspace_bytes(int cap, int D) { return count_offset_floats(cap, D) * 4 + (size_t)2 * kGrid * 8; }
 
 // ------------------------------------------------------------------ PTX wrappers
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-               ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(acc) : "memory");
+// D (+)= A B.  a, b: low words of the descriptors (start address, leading offset), their high words are the same for all operands here.  The
+// one thread that issues them has few instructions between two products: the descriptors' parts are added up from constants.
+constexpr uint32_t kDescHigh = (128u >> 4) | (1u << 14);       // octets of rows 128 bytes apart, version 1, no swizzle
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t lb) { return ((addr >> 4) & 0x3FFFu) | ((lb >> 4) << 16); }
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t acc) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-               ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(acc) : "memory");
+template <bool ACC>
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t id) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "r"(b), "r"(id), "n"(ACC ? 1 : 0), "n"(kDescHigh) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t id, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 y, {%2, %5};\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "r"(b), "r"(id), "r"(acc), "n"(kDescHigh) : "memory");
 }
 #define KVQ_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
 #define KVQ_W8(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
@@ -108,6 +123,11 @@ __device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t sel
   asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(sel));
   return d;
 }
+__device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+  return d;
+}
 __device__ __forceinline__ bool bar_any(int id, int nthreads, bool p) {
   uint32_t r;
   __syncwarp();
@@ -117,14 +137,31 @@ __device__ __forceinline__ bool bar_any(int id, int nthreads, bool p) {
 }
 
 // Token of a page's block of 32 that stands at place k of its 32 columns: codes of four tokens share a word, those of two halves a load.
-__host__ __device__ constexpr int token_at(int k) { return 16 * ((k & 7) >> 2) + 2 * (k >> 3) + ((k & 3) >> 1) + 8 * (k & 1); }
-__host__ __device__ constexpr int place_of(int u) { return 8 * ((u & 7) >> 1) + 4 * (u >> 4) + 2 * (u & 1) + ((u >> 3) & 1); }
+__host__ __device__ constexpr int token_at(int k) { return 16 * ((k & 7) >> 2) + 2 * (k >> 3) + (k & 1) + 8 * ((k >> 1) & 1); }
 
-// Code bytes lo, hi of a word as fp16 numbers times scale plus zero-point, one rounding (byte -> 0x64bb = 1024 + code, minus 1024: exact).
-__device__ __forceinline__ uint32_t values2(uint32_t bytes, uint32_t sel, __half2 s, __half2 z) {
-  const __half2 code = __hsub2(as_h2(permute(bytes, 0x64646464u, sel)), __half2half2(__ushort_as_half(0x6400)));
-  return as_u32(__hfma2(code, s, z));
-}
+// Two codes of a field of a word's bytes 0 and 2 (of w >> 8: bytes 1 and 3) as fp16 numbers times scale plus zero-point, one rounding.  The
+// field stays where it stands: under the bits of 1024 it reads 1024 + code 2^(B f), which one operation makes the code, exactly.
+// The constants are held in registers (the compiler would make them again for every use).
+template <int B>
+struct Codes {
+  static constexpr int F = 8 / B;
+  uint32_t magic, up[F], bias[F];
+  __device__ __forceinline__ Codes() {
+    asm volatile("mov.b32 %0, 0x64006400;" : "=r"(magic));
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+      const uint32_t u = as_u32(__float2half2_rn(1.0f / (float)(1 << (B * f)))), v = as_u32(__float2half2_rn(-1024.0f / (float)(1 << (B * f))));
+      asm volatile("mov.b32 %0, %1;" : "=r"(up[f]) : "r"(u));
+      asm volatile("mov.b32 %0, %1;" : "=r"(bias[f]) : "r"(v));
+    }
+  }
+  __device__ __forceinline__ uint32_t values(uint32_t w, int f, __half2 s, __half2 z) const {
+    const uint32_t mask = (((1u << B) - 1u) << (B * f)) * 0x00010001u;
+    const __half2 raw = as_h2((w & mask) | magic);
+    const __half2 code = f == 0 ? __hadd2(raw, as_h2(bias[0])) : __hfma2(raw, as_h2(up[f]), as_h2(bias[f]));
+    return as_u32(__hfma2(code, s, z));
+  }
+};
 
 // A tile: its rows, and the pages that they see.
 struct Tile {
@@ -132,7 +169,6 @@ struct Tile {
   int n, rows, first, pairs;   // of the sequence
   SeenPages seen;
 };
-struct Share { long long lo, hi; int b, h, i, page; };       // of a CTA: positions on the axis, tile and page of the first
 
 template <int D, int KB, int VB>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -144,13 +180,15 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
   constexpr int NI = D / 32;
   extern __shared__ __align__(128) uint8_t smem[];
   const Smem sl = smem_of<D>(g.B);
-  long long* sPref = reinterpret_cast<long long*>(smem + sl.pref);      // (tile, page) pairs in front of every sequence
+  long long* sPref = reinterpret_cast<long long*>(smem + sl.pref);      // (tile, page) pairs and gaps in front of every sequence
   int* sSeq = reinterpret_cast<int*>(smem + sl.seq);                    // tokens, rows, first row
-  int* sMisc = reinterpret_cast<int*>(smem + sl.misc);                  // [0] abort [1] tensor memory [2, 3] counts returned [4..7] pages of big values [8..11] share
+  int* sMisc = reinterpret_cast<int*>(smem + sl.misc);                  // [0] abort [1] tensor memory [2, 3] counts returned [4..7] share [8..11] pages of big keys [12..15] ... of big values
   volatile int* abort_flag = sMisc;
-  volatile int* sBig = sMisc + 4;
+  volatile int* sBig = sMisc + 8;           // by page: keys, then values
   const int tid_ = threadIdx.x, lane = tid_ & 31, warp = __shfl_sync(FULL, tid_ >> 5, 0);
   const int B = g.B, G = g.G, Hkv = g.Hkv;
+  const uint32_t inv_g = G > 1 ? 0xFFFFFFFFu / (uint32_t)G + 1u : 0u;
+  auto by_g = [&](int x) { return G > 1 ? (int)__umulhi((uint32_t)x, inv_g) : x; };      // x / G, exact up to 2^29
   // barriers: key tile full / empty [2], value tile full / empty [2], queries [2], S [2], P [2], O [2], drain
   const uint32_t bar = smem_u32(smem + sl.bars);
   const uint32_t bKF = bar, bKE = bar + 16, bVF = bar + 32, bVE = bar + 48, bQ = bar + 64, bS = bar + 80, bP = bar + 96, bO = bar + 112, bDrain = bar + 128;
@@ -158,21 +196,20 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
   if (tid_ == 0) {
     sMisc[0] = 0;
     for (int k = 0; k < 2; ++k) {
-      mbar_init(bKF + 8 * k, 4); mbar_init(bKE + 8 * k, 1); mbar_init(bVF + 8 * k, 4); mbar_init(bVE + 8 * k, 1);
+      mbar_init(bKF + 8 * k, 8); mbar_init(bKE + 8 * k, 1); mbar_init(bVF + 8 * k, 8); mbar_init(bVE + 8 * k, 1);
       mbar_init(bQ + 8 * k, 4); mbar_init(bS + 8 * k, 1); mbar_init(bP + 8 * k, 4); mbar_init(bO + 8 * k, 1);
     }
     mbar_init(bDrain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   begin_after_predecessor();
-  if (warp == 12) {
+  if (warp == 24) {
     tc::tmem_alloc(smem_u32(&sMisc[1]), kTmemCols);
     tc::tmem_relinquish();
   }
   // ---- plan: (tile, page) pairs per sequence, this CTA's share
   auto seen_by = [&](int n, int rows, int pairs, int i) {
-    const int r0 = i * kTile / G, r1 = min(i * kTile + kTile, pairs) - 1;
-    return seen_pages(n - rows + r0, n - rows + r1 / G, p.window, p.sinks);
+    return seen_pages(n - rows + by_g(i * kTile), n - rows + by_g(min(i * kTile + kTile, pairs) - 1), p.window, p.sinks);
   };
   for (int b = warp; b < B; b += kThreads / 32) {
     bool bad;
@@ -180,7 +217,7 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
     if (bad && lane == 0) atomicOr(p.status, KVQ_STATUS_BAD_INPUT);
     const int pairs = s.rows * G;
     long long sum = 0;
-    for (int i = lane; i * kTile < pairs; i += 32) sum += seen_by(s.n, s.rows, pairs, i).count;
+    for (int i = lane; i * kTile < pairs; i += 32) sum += seen_by(s.n, s.rows, pairs, i).count + kGap;
     for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(FULL, sum, off);
     if (lane == 0) {
       sPref[b + 1] = sum * Hkv;
@@ -221,11 +258,11 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
     const long long per_head = (sPref[lo + 1] - sPref[lo]) / Hkv;
     const int h = (int)((x_lo - sPref[lo]) / per_head);
     long long rest = x_lo - sPref[lo] - h * per_head;
-    int i0 = 0, page = 0, tile = 0;
+    int i0 = 0, tile = 0;
     bool found = false;
     for (; !found && i0 * kTile < pairs; i0 += 32) {
       const int i = i0 + lane;
-      const long long own = i * kTile < pairs ? seen_by(n, rows, pairs, i).count : 0;
+      const long long own = i * kTile < pairs ? seen_by(n, rows, pairs, i).count + kGap : 0;
       long long v = own;
       for (int off = 1; off < 32; off <<= 1) {
         const long long u = __shfl_up_sync(FULL, v, off);
@@ -234,14 +271,14 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       const uint32_t beyond = __ballot_sync(FULL, v > rest);
       if (beyond) {
         const int src = __ffs(beyond) - 1;
-        page = (int)(rest - __shfl_sync(FULL, v - own, src));
+        rest -= __shfl_sync(FULL, v - own, src);
         tile = i0 + src;
         found = true;
       } else {
         rest -= __shfl_sync(FULL, v, 31);
       }
     }
-    if (lane == 0) { sMisc[8] = lo; sMisc[9] = h; sMisc[10] = tile; sMisc[11] = page; }
+    if (lane == 0) { sMisc[4] = lo; sMisc[5] = h; sMisc[6] = tile; sMisc[7] = (int)rest; }
   }
   __syncthreads();
 
@@ -264,25 +301,50 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
     }
     return tile_of(min(b, B - 1), h, i);
   };
-  // Segments: the pages of one tile that lie in the share.  each(tile, first page, pages).
-  auto segments = [&](auto&& each) {
-    if (x_lo >= x_hi) return;
-    Tile t = tile_of(sMisc[8], sMisc[9], sMisc[10]);
-    int page = sMisc[11];
-    for (long long x = x_lo; x < x_hi;) {
-      const int pages = (int)min((long long)(t.seen.count - page), x_hi - x);
-      each(t, page, pages, x);
-      x += pages;
-      page = 0;
-      if (x < x_hi) t = next_tile(t);
+  // The share, segment by segment: pages page .. end - 1 of tile t, which starts at xs on the axis (a gap, then its pages).
+  struct Cursor { Tile t; long long xs; int page, end; bool on; };
+  auto settle = [&](Cursor& c) {                     // on to the first tile from c.t on of which a page lies in the share
+    while (true) {
+      const long long lo = x_lo - c.xs - kGap, hi = x_hi - c.xs - kGap;
+      c.page = lo > 0 ? (int)lo : 0;
+      c.end = hi < c.t.seen.count ? (int)hi : c.t.seen.count;
+      c.on = c.end > c.page;
+      if (c.on) return;
+      c.xs += kGap + c.t.seen.count;
+      if (c.xs + kGap >= x_hi) return;
+      c.t = next_tile(c.t);
+    }
+  };
+  auto start = [&]() {
+    Cursor c;
+    c.on = false;
+    if (x_lo >= x_hi) return c;
+    c.t = tile_of(sMisc[4], sMisc[5], sMisc[6]);
+    c.xs = x_lo - sMisc[7];
+    settle(c);
+    return c;
+  };
+  auto advance = [&](Cursor& c) {                    // to the next segment
+    c.xs += kGap + c.t.seen.count;
+    c.on = c.xs + kGap < x_hi;
+    if (c.on) {
+      c.t = next_tile(c.t);
+      settle(c);
     }
   };
   bool aborted = false;
-  // A wait of a whole warp; after a time-out the role goes on without waiting.
+  // A wait of a whole warp; after a time-out the role goes on without waiting.  Most waits are long: a look costs three instructions, the clock
+  // and the other roles' failure are looked at now and then.
   auto wait_warp = [&](uint32_t b, uint32_t parity) {
     if (aborted) return;
     if (__all_sync(FULL, mbar_try_wait(b, parity))) return;
-    const bool got = tc::wait_or_abort(b, parity, wait_ns, abort_flag);
+    bool got = false;
+    const unsigned long long t0 = globaltimer_ns();
+    while (true) {
+#pragma unroll 1
+      for (int n = 0; n < 32 && !got; ++n) got = mbar_try_wait_hint(b, parity, 1000u);
+      if (got || *abort_flag || globaltimer_ns() - t0 > wait_ns) break;
+    }
     if (!__all_sync(FULL, got)) {
       aborted = true;
       *abort_flag = 1;
@@ -292,6 +354,7 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
   };
 
   if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     // =========================================================== softmax: half w of the tile, a thread per row
     const int w = warp >> 2, row = tid_ & 127;
     const uint32_t tS = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColS + 128 * w, tO = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColO + 128 * w;
@@ -299,26 +362,30 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
     const unsigned long long id40 = (call_id & 0xFFFFFFFFFFull) ? (call_id & 0xFFFFFFFFFFull) : 1ull;
     unsigned long long* counts = reinterpret_cast<unsigned long long*>(ws + count_offset_floats(cap, D));
     int it = 0, done = 0, seg = 0;                   // pages of the share so far, those that this half had, segments it had
-    segments([&](const Tile& t, int page0, int pages, long long x) {
+#pragma unroll 1
+    for (Cursor c = start(); c.on; advance(c)) {
+      const Tile& t = c.t;
+      const int page0 = c.page, pages = c.end - c.page;
       const int pair0 = t.i * kTile + 128 * w;
-      if (pair0 >= t.pairs) { it += pages; return; }
+      if (pair0 >= t.pairs) { it += pages; continue; }
       // ---- the row's query: fp16 in the order of the key tiles' channels, scaled to at most 2^15 in size
-      const int pair = pair0 + row, r = min(pair, t.pairs - 1) / G;
+      const int pair = pair0 + row, r = by_g(min(pair, t.pairs - 1));
       const bool real = pair < t.pairs;
       float f = c1;
       {
         const uint16_t* src = q + ((size_t)(t.first + r) * g.Hq + (size_t)t.h * G + (pair - r * G)) * D;
-        uint32_t qw[D / 2];
-        uint32_t top = 0;
+        uint32_t qw[D / 2];                          // (the whole row at once: one wait for memory)
 #pragma unroll
         for (int k = 0; k < D / 8; ++k) {
           uint4 v = make_uint4(0u, 0u, 0u, 0u);
           if (real) v = *reinterpret_cast<const uint4*>(src + 8 * k);
           qw[4 * k] = v.x; qw[4 * k + 1] = v.y; qw[4 * k + 2] = v.z; qw[4 * k + 3] = v.w;
-          top = __vmaxu2(__vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)), top);
         }
+        // |q| has the order of its 16-bit pattern: bf16 rows are scaled to bring the exponent of the largest to that of one
         if (g.in_dtype == KVQ_BF16) {
-          // |q| has the exponent of its 16-bit pattern: bring the largest to 2^0 .. 2^1
+          uint32_t top = 0;
+#pragma unroll
+          for (int k = 0; k < D / 2; ++k) top = __vmaxu2(top, qw[k] & 0x7FFF7FFFu);
           const int e = (int)(max(top & 0xFFFFu, top >> 16) >> 7);
           const int shift = e == 0 ? 0 : min(max(127 - e, -126), 126);
           const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
@@ -327,11 +394,12 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
           for (int k = 0; k < D / 2; ++k)
             qw[k] = as_u32(__floats2half2_rn(__uint_as_float(qw[k] << 16) * up, __uint_as_float(qw[k] & 0xFFFF0000u) * up));
         }
-        // chunk 4 i + ch: channels 32 i + 4 ch + {0..3}, then those 16 further
+        // chunk 4 i + ch: channels 32 i + 4 ch + {0, 2, 1, 3}, then those 16 further
 #pragma unroll
         for (int k = 0; k < D / 8; ++k) {
           const int i = k >> 2, ch = k & 3, a = (32 * i + 4 * ch) / 2;
-          *reinterpret_cast<uint4*>(sq + k * T::kLbQ) = make_uint4(qw[a], qw[a + 1], qw[a + 8], qw[a + 9]);
+          *reinterpret_cast<uint4*>(sq + k * T::kLbQ) = make_uint4(permute(qw[a], qw[a + 1], 0x5410u), permute(qw[a], qw[a + 1], 0x7632u),
+                                                                   permute(qw[a + 8], qw[a + 9], 0x5410u), permute(qw[a + 8], qw[a + 9], 0x7632u));
         }
       }
       tc::fence_async_smem();
@@ -340,7 +408,7 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       if (lane == 0) mbar_arrive(bQ + 8 * w);
       // ---- what the rows see
       const int pos = t.n - t.rows + r, lim = pos + 1, low = p.window > 0 ? max(lim - p.window, 0) : 0;
-      const int r_first = pair0 / G, r_last = (min(pair0 + 128, t.pairs) - 1) / G;
+      const int r_first = by_g(pair0), r_last = by_g(min(pair0 + 128, t.pairs) - 1);
       const int lim_all = t.n - t.rows + r_first + 1, low_all = p.window > 0 ? max(t.n - t.rows + r_last + 1 - p.window, 0) : 0;
       float m = -INFINITY;
       f32x2 l2 = pack2(0.f, 0.f);
@@ -348,95 +416,82 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       for (int j = 0; j < pages; ++j, ++it, ++done) {
         wait_warp(bS + 8 * w, done & 1);
         tc::tc_fence_after();
-        const bool big = sBig[it & 3] != 0;
-        const float fs = big ? f * kBigUp : f;
+        wait_warp(bVF + 8 * (it & 1), (it >> 1) & 1);          // (there by now: the values' tile and whether it is scaled)
+        const bool big = sBig[4 + (it & 3)] != 0;
+        const float fs = sBig[it & 3] != 0 ? f * kBigUp : f;
         const int tok = t.seen.logical(page0 + j) * kPageTokens;
         const bool open = tok + kPageTokens <= lim_all && (tok >= low_all || tok + kPageTokens <= p.sinks);       // every row sees the whole page
         const int lim_t = lim - tok, low_t = low - tok, sink_t = p.sinks - tok;
-        auto sees = [&](int c, int k) {              // column 32 c + k
-          const int u = 32 * c + token_at(k);
-          return u < lim_t && (u >= low_t || u < sink_t);
-        };
-        auto page_pass = [&](auto masked_tag) {
-          constexpr bool MASKED = decltype(masked_tag)::value;
-          uint32_t a[32], b[32];
-          float top = -INFINITY;
-          auto max_of = [&](const uint32_t (&s)[32], int c) {
-            float t0 = -INFINITY, t1 = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < 32; k += 2) {
-              float x0 = __uint_as_float(s[k]), x1 = __uint_as_float(s[k + 1]);
-              if (MASKED) { if (!sees(c, k)) x0 = -INFINITY; if (!sees(c, k + 1)) x1 = -INFINITY; }
-              t0 = fmaxf(t0, x0); t1 = fmaxf(t1, x1);
-            }
-            top = fmaxf(top, fmaxf(t0, t1));
-          };
-          tmem_ld32(tS, a);
-          wait_ld(a);
-          tmem_ld32(tS + 32, b);
-          max_of(a, 0);
-          wait_ld(b);
-          tmem_ld32(tS + 64, a);
-          max_of(b, 1);
-          wait_ld(a);
-          tmem_ld32(tS + 96, b);
-          max_of(a, 2);
-          wait_ld(b);
-          tmem_ld32(tS, a);                          // the second pass's first columns are on their way
-          max_of(b, 3);
-          top *= fs;
-          // ---- the reference moves when a logit passes it by the headroom
-          const bool move = top > m + kHeadroom;     // (m = -inf: any logit at all)
-          if (__any_sync(FULL, move)) {
-            const float nm = move ? top : m;
-            const float keep = m == -INFINITY ? 0.f : ex2(m - nm);       // (no logit yet: nothing but zeros in O)
-            if (j > 0) {
-              // (nobody writes O now: this page's product has not been asked for, and S arrived behind the last one's.  a is waited for first.)
-              wait_ld(a);
+        uint32_t a[32];
+        if (!open) {
+          // what a row does not see becomes -infinity where it stands (pages at a mask's edge; the code below has no conditions)
 #pragma unroll 1
-              for (int c = 0; c < D / 32; ++c) {
-                tmem_ld32(tO + 32 * c, b);
-                wait_ld(b);
+          for (int c = 0; c < 4; ++c) {
+            tmem_ld32(tS + 32 * c, a);
+            wait_ld(a);
 #pragma unroll
-                for (int k = 0; k < 32; ++k) b[k] = __float_as_uint(__uint_as_float(b[k]) * keep);
-                tmem_st32(tO + 32 * c, b);
-              }
+            for (int k = 0; k < 32; ++k) {
+              const int u = 32 * c + token_at(k);
+              const bool hidden = (u >= lim_t) | ((u < low_t) & (u >= sink_t));      // (no branches)
+              a[k] = hidden ? 0xFF800000u : a[k];
             }
-            l2 = mul2(l2, pack2(keep, keep));
-            m = nm;
+            tmem_st32(tS + 32 * c, a);
           }
-          // ---- weights: 2^(x - m), fp16, where S was (columns that this warp has read); pages of big values carry P times 2^10
-          const float base = m == -INFINITY ? 0.f : m;
-          const f32x2 f2 = pack2(fs, fs), nb = pack2(-base, -base);
-          f32x2 sum = pack2(0.f, 0.f);
-          auto weigh = [&](const uint32_t (&s)[32], int c) {
-            uint32_t w16[16];
+          tc::tc_wait_st();
+        }
+        float top = -INFINITY;
+#pragma unroll 1
+        for (int c = 0; c < 128; c += 32) {
+          tmem_ld32(tS + c, a);
+          wait_ld(a);
+          float t0 = max3(top, a[0], a[1]), t1 = __uint_as_float(a[2]);
 #pragma unroll
-            for (int k = 0; k < 32; k += 2) {
-              const float2 e = unpack2(fma2(pack2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), f2, nb));
-              float2 pr = make_float2(ex2(e.x), ex2(e.y));
-              if (MASKED) { if (!sees(c, k)) pr.x = 0.f; if (!sees(c, k + 1)) pr.y = 0.f; }
-              sum = add2(sum, pack2(pr.x, pr.y));
-              if (big) { pr.x *= kBigUp; pr.y *= kBigUp; }
-              w16[k / 2] = as_u32(__floats2half2_rn(pr.x, pr.y));
+          for (int k = 3; k < 31; k += 4) { t0 = max3(t0, a[k], a[k + 1]); t1 = max3(t1, a[k + 2], a[k + 3]); }
+          top = max3(t0, __float_as_uint(t1), a[31]);
+        }
+        top *= fs;
+        // ---- the reference moves when a logit passes it by the headroom
+        const bool move = top > m + kHeadroom;       // (m = -inf: any logit at all)
+        if (__any_sync(FULL, move)) {
+          const float nm = move ? top : m;
+          const float keep = m == -INFINITY ? 0.f : ex2(m - nm);         // (no logit yet: nothing but zeros in O)
+          if (j > 0) {
+            // (nobody writes O now: this page's product has not been asked for, and S arrived behind the last one's)
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+              tmem_ld32(tO + c, a);
+              wait_ld(a);
+#pragma unroll
+              for (int k = 0; k < 32; ++k) a[k] = __float_as_uint(__uint_as_float(a[k]) * keep);
+              tmem_st32(tO + c, a);
             }
-            tmem_st16(tS + 16 * c, w16);
-          };
-          wait_ld(a);
-          tmem_ld32(tS + 32, b);
-          weigh(a, 0);
-          wait_ld(b);
-          tmem_ld32(tS + 64, a);
-          weigh(b, 1);
-          wait_ld(a);
-          tmem_ld32(tS + 96, b);
-          weigh(a, 2);
-          wait_ld(b);
-          weigh(b, 3);
-          l2 = add2(l2, sum);
+          }
+          l2 = mul2(l2, pack2(keep, keep));
+          m = nm;
+        }
+        // ---- weights: 2^(x - m), fp16, where S was (columns that this warp has read); pages of big values carry P times 2^10
+        const float base = (m == -INFINITY ? 0.f : m) - (big ? 10.0f : 0.0f);
+        const f32x2 f2 = pack2(fs, fs), nb = pack2(-base, -base);
+        f32x2 sum = pack2(0.f, 0.f);
+        auto weigh = [&](const uint32_t (&s)[32], uint32_t to) {
+          uint32_t w16[16];
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) {
+            const float2 e = unpack2(fma2(pack2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), f2, nb));
+            const float2 pr = make_float2(ex2(e.x), ex2(e.y));
+            sum = add2(sum, pack2(pr.x, pr.y));
+            w16[k / 2] = as_u32(__floats2half2_rn(pr.x, pr.y));
+          }
+          tmem_st16(to, w16);
         };
-        if (open) page_pass(std::false_type{});
-        else page_pass(std::true_type{});
+#pragma unroll 1
+        for (int c = 0; c < 128; c += 32) {
+          tmem_ld32(tS + c, a);
+          wait_ld(a);
+          weigh(a, tS + (c >> 1));
+        }
+        const float back = big ? kBigDown : 1.0f;
+        l2 = fma2(sum, pack2(back, back), l2);
         tc::tc_wait_st();
         tc::tc_fence_before();
         __syncwarp();
@@ -447,40 +502,64 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       ++seg;
       tc::tc_fence_after();
       const float l = unpack2(l2).x + unpack2(l2).y;
-      const long long xs = x - page0;                // where the tile starts on the axis
       const bool whole = page0 == 0 && pages == t.seen.count;
       const float inv = whole ? (l > 0.f ? 1.0f / l : 0.f) : 1.0f;
-      const size_t oi = ((size_t)(t.first + r) * g.Hq + (size_t)t.h * G + (pair - r * G)) * D;
       const int slot = 2 * (int)blockIdx.x + (page0 == 0 ? 1 : 0), cr = 128 * w + row;      // (page0 > 0: the tile started in another share)
-      float* po = ws + ((size_t)slot * cap + cr) * D;
+      // Rows leave through the warp's part of the query tile (done with), so that a store covers whole rows: piece k of 16 bytes of row r
+      // goes to place (r + k) % 32 of its 32, which neither the rows' nor the pieces' order makes collide.
+      {
+        const long long out_row = (long long)(t.first + r) * g.Hq + (long long)t.h * G + (pair - r * G);
+        const int wr = row & ~31, rows_here = min(32, t.pairs - pair0 - wr);         // (may be none)
+        uint8_t* stage = smem + sl.q + w * T::kQ + wr * 16;
+        const bool wide = !whole || out_dtype == KVQ_FP32;                           // rows of 4 D bytes: two rounds
 #pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
-        uint32_t a[32];
-        tmem_ld32(tO + 32 * c, a);
-        wait_ld(a);
-        if (!real) continue;
-        if (whole && out_dtype != KVQ_FP32) {
+        for (int c0 = 0; c0 < D; c0 += wide ? D / 2 : D) {
+#pragma unroll 1
+          for (int cc = 0; cc < (wide ? D / 2 : D); cc += 32) {
+            uint32_t a[32];
+            tmem_ld32(tO + c0 + cc, a);
+            wait_ld(a);
+            if (wide) {
 #pragma unroll
-          for (int k = 0; k < 32; k += 8) {
-            uint32_t o4[4];
+              for (int k = 0; k < 8; ++k) {
+                const int piece = cc / 4 + k;
+                *reinterpret_cast<float4*>(stage + piece * T::kLbQ + ((lane + piece) & 31) * 16) =
+                    make_float4(__uint_as_float(a[4 * k]) * inv, __uint_as_float(a[4 * k + 1]) * inv, __uint_as_float(a[4 * k + 2]) * inv, __uint_as_float(a[4 * k + 3]) * inv);
+              }
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              o4[e] = (uint32_t)f32_to_bits16(__uint_as_float(a[k + 2 * e]) * inv, out_dtype) |
-                      ((uint32_t)f32_to_bits16(__uint_as_float(a[k + 2 * e + 1]) * inv, out_dtype) << 16);
-            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + oi + 32 * c + k) = make_uint4(o4[0], o4[1], o4[2], o4[3]);
+              for (int k = 0; k < 4; ++k) {
+                const int piece = cc / 8 + k;
+                uint32_t o4[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  o4[e] = (uint32_t)f32_to_bits16(__uint_as_float(a[8 * k + 2 * e]) * inv, out_dtype) |
+                          ((uint32_t)f32_to_bits16(__uint_as_float(a[8 * k + 2 * e + 1]) * inv, out_dtype) << 16);
+                *reinterpret_cast<uint4*>(stage + piece * T::kLbQ + ((lane + piece) & 31) * 16) = make_uint4(o4[0], o4[1], o4[2], o4[3]);
+              }
+            }
           }
-        } else {
-          float* dst = whole ? static_cast<float*>(out) + oi : po;
-#pragma unroll
-          for (int k = 0; k < 32; k += 4)
-            *reinterpret_cast<float4*>(dst + 32 * c + k) = make_float4(__uint_as_float(a[k]) * inv, __uint_as_float(a[k + 1]) * inv,
-                                                                       __uint_as_float(a[k + 2]) * inv, __uint_as_float(a[k + 3]) * inv);
+          __syncwarp();
+          constexpr int NP = D / 8;                  // pieces of a row and round
+          // (all lanes go round as often: they ask each other where a row goes)
+#pragma unroll 4
+          for (int i = 0; i < rows_here * NP; i += 32) {
+            const int idx = min(i + lane, rows_here * NP - 1);
+            const int rr = idx / NP, piece = idx % NP;
+            const uint4 v = *reinterpret_cast<const uint4*>(stage + piece * T::kLbQ + ((rr + piece) & 31) * 16);
+            uint8_t* dst;
+            const long long orow = __shfl_sync(FULL, out_row, rr);
+            if (whole) dst = static_cast<uint8_t*>(out) + (orow * D + c0) * (wide ? 4 : 2);
+            else dst = reinterpret_cast<uint8_t*>(ws + ((size_t)slot * cap + 128 * w + wr + rr) * D + c0);
+            *reinterpret_cast<uint4*>(dst + 16 * piece) = v;
+          }
+          __syncwarp();
         }
       }
       tc::tc_fence_before();
-      if (whole) return;
+      if (whole) continue;
       if (real) *reinterpret_cast<float2*>(ws + ml_offset_floats(cap, D) + ((size_t)slot * cap + cr) * 2) = make_float2(m, l);
-      const int first = plan.cta_of(xs), parts = plan.cta_of(xs + t.seen.count - 1) - first + 1;
+      const int first = plan.cta_of(c.xs + kGap), parts = plan.cta_of(c.xs + kGap + t.seen.count - 1) - first + 1;
       __threadfence();
       named_bar_sync(1 + w, 128);
       if (row == 0) const_cast<volatile int*>(sMisc)[2 + w] = (int)tagged_count(counts + 2 * first + w, id40);
@@ -522,7 +601,8 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
             ms = mb;
           }
           const float iv = den > 0.f ? 1.0f / den : 0.f;
-          const size_t at = ((size_t)(t.first + pr / G) * g.Hq + (size_t)t.h * G + pr % G) * D + 4 * c4;
+          const int rw = by_g(pr);
+          const size_t at = ((size_t)(t.first + rw) * g.Hq + (size_t)t.h * G + (pr - rw * G)) * D + 4 * c4;
           if (out_dtype == KVQ_FP32) {
             *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(num.x * iv, num.y * iv, num.z * iv, num.w * iv);
           } else {
@@ -535,123 +615,129 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
         if (row == 0) counts[2 * first + w] = 0ull;
       }
       named_bar_sync(1 + w, 128);
-    });
-  } else if (warp < 12) {
-    // =========================================================== pages to 16-bit tiles: warp `blk` takes a block of 32 tokens
-    const int blk = warp - 8;
+    }
+  } else if (warp < 24) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsTiles));
+    // =========================================================== pages to 16-bit tiles: two warps take a block of 32 tokens (one is bound by latency)
+    const int blk = warp & 3, half = (warp >> 2) & 1;
     const int ngk = D / g.gk, ngv = D / g.gv;
-    const int tl = lane >> 2, ch = lane & 3;         // keys: token of a pass, quarter of its row
-    constexpr int KCB = (KW < 4 ? KW : 4) * 4;
-    uint32_t kw[4][KW], km[4], vm[4];
-    uint4 vw[NMW];
-    // token (of 32) that lane group tl of pass k takes: neighbours in place, for writes without bank conflicts
-    auto pass_token = [&](int k) { return (tl >> 1) + 8 * (tl & 1) + 4 * (k & 1) + 16 * (k >> 1); };
+    // The page to load is one ahead of the one that is written, its number was read a page earlier still.
     const uint8_t* page_ptr = nullptr;
-    auto find = [&](const Tile& t, int i) {          // the page's address
-      int id = pool_page(p, t.b, t.seen.logical(i));
-      if (id < 0) {
+    Cursor nc = start();
+    int nid = 0, tokens = 0;                         // of the page at page_ptr: tokens of this warp's block that the sequence holds
+    auto look_up = [&]() { if (nc.on) nid = p.table[(long long)nc.t.b * p.table_stride + nc.t.seen.logical(nc.page)]; };
+    auto to_next = [&]() {                           // address of the page whose number is there, and on to the number of the one behind
+      int id = nid;
+      if ((unsigned)id >= (unsigned)p.n_pool) {      // outside the pool: another page is read in its place
         if (lane == 0) atomicOr(p.status, KVQ_STATUS_BAD_INPUT);
         id = 0;
       }
-      page_ptr = p.pages + ((size_t)id * Hkv + t.h) * (size_t)g.page_bytes;
+      page_ptr = p.pages + ((size_t)id * Hkv + nc.t.h) * (size_t)g.page_bytes;
+      tokens = nc.t.n - nc.t.seen.logical(nc.page) * kPageTokens - 32 * blk;
+      if (++nc.page == nc.end) advance(nc);
+      look_up();
     };
-    auto load_keys = [&]() {
+    look_up();
+    // Scales and zero-points of the lane's token, a word per group; nothing of tokens that the sequence does not hold (their bytes are
+    // anything).  True where a value may pass half the fp16 range.
+    auto load_meta = [&](uint32_t (&m)[4], int off, int count) {
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(page_ptr + off) + (32 * blk + lane) * count;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) load_words<KW>(page_ptr + (size_t)(32 * blk + pass_token(k)) * (D * KB / 8) + ch * KCB, 64, kw[k]);
-      const uint32_t* m = reinterpret_cast<const uint32_t*>(page_ptr + g.k_meta_off) + (32 * blk + lane) * ngk;
-#pragma unroll
-      for (int j = 0; j < NI; ++j) if (j < ngk) km[j] = m[j];
+      for (int e = 0; e < NI; ++e) if (e < count) m[e] = src[e];
     };
-    auto load_values = [&]() {
-      const uint8_t* v = page_ptr + g.v_codes_off + blk * (4 * D * VB) + lane * 16;
+    auto check_meta = [&](uint32_t (&m)[4], int count, float qmax, bool there) {
+      bool wide = false;
 #pragma unroll
-      for (int mw = 0; mw < NMW; ++mw) vw[mw] = *reinterpret_cast<const uint4*>(v + 512 * mw);
-      const uint32_t* m = reinterpret_cast<const uint32_t*>(page_ptr + g.v_meta_off) + (32 * blk + lane) * ngv;
-#pragma unroll
-      for (int j = 0; j < NI; ++j) if (j < ngv) vm[j] = m[j];
-    };
-    // The next page to load: one ahead of the one that is written.
-    Tile nt{};
-    int npage = 0;
-    long long nx = x_lo;
-    auto step = [&]() {                              // to the page behind
-      ++nx;
-      if (++npage == nt.seen.count) {
-        npage = 0;
-        if (nx < x_hi) nt = next_tile(nt);
-      }
-      if (nx < x_hi) find(nt, npage);
-    };
-    if (x_lo < x_hi) {
-      nt = tile_of(sMisc[8], sMisc[9], sMisc[10]);
-      npage = sMisc[11];
-      find(nt, npage);
-      load_keys();
-      load_values();
-    }
-    int it = 0;
-    segments([&](const Tile& t, int page0, int pages, long long x) {
-#pragma unroll 1
-      for (int j = 0; j < pages; ++j, ++it) {
-        const int buf = it & 1, tok = t.seen.logical(page0 + j) * kPageTokens + 32 * blk;
-        // scales and zero-points of this lane's token; nothing of tokens that the sequence does not hold (their bytes are anything)
-        bool wide = false;
-        auto checked = [&](uint32_t (&m)[4], int count, float qmax) {
-#pragma unroll
-          for (int e = 0; e < NI; ++e) {
-            if (e < count) {
-              if (tok + lane >= t.n) m[e] = 0u;
-              const float2 sz = __half22float2(as_h2(m[e]));
-              wide |= fabsf(sz.y) > 32752.0f || sz.x * qmax > 32752.0f;
-            }
-          }
-        };
-        checked(km, ngk, (float)((1 << KB) - 1));
-        checked(vm, ngv, (float)((1 << VB) - 1));
-        const bool big = bar_any(3, 128, wide);
-        if (big) {
-          const __half2 down = __float2half2_rn(kBigDown);
-#pragma unroll
-          for (int e = 0; e < NI; ++e) {
-            if (e < ngk) km[e] = as_u32(__hmul2(as_h2(km[e]), down));
-            if (e < ngv) vm[e] = as_u32(__hmul2(as_h2(vm[e]), down));
-          }
+      for (int e = 0; e < NI; ++e) {
+        if (e < count) {
+          if (!there) m[e] = 0u;
+          const float2 sz = __half22float2(as_h2(m[e]));
+          wide |= fabsf(sz.y) > 32752.0f || sz.x * qmax > 32752.0f;
         }
-        if (it >= 2) wait_warp(bKE + 8 * buf, ((it >> 1) - 1) & 1);
-        if (warp == 8 && lane == 0) sBig[it & 3] = big;
-        {
+      }
+      return wide;
+    };
+    auto scale_meta = [&](uint32_t (&m)[4], int count) {
+#pragma unroll
+      for (int e = 0; e < NI; ++e) if (e < count) m[e] = as_u32(__hmul2(as_h2(m[e]), __float2half2_rn(kBigDown)));
+    };
+    int it = 0;
+    if (warp < 16) {
+      // ------------------------------------------------------------ keys: half of the passes of eight tokens
+      const int tl = lane & 7, ch = lane >> 3;       // token of a pass of eight (neighbours in place), quarter of its row
+      constexpr int KCB = (KW < 4 ? KW : 4) * 4;
+      const Codes<KB> kc;
+      const int skip_it = (int)blockIdx.x == (int)(skip_x >> 8) && skip_x >= 0 ? (int)(skip_x & 255) : -1;      // (test hook: page skip_x % 256 of CTA skip_x / 256 never arrives)
+      uint32_t kw[2][KW], km[4] = {0u, 0u, 0u, 0u};
+      auto load = [&]() {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) load_words<KW>(page_ptr + (32 * blk + token_at(8 * k + 16 * half + tl)) * (D * KB / 8) + ch * KCB, 64, kw[k]);
+        load_meta(km, g.k_meta_off, ngk);
+      };
+      bool more = nc.on;
+      if (more) { to_next(); load(); }
+#pragma unroll 1
+      for (; more; ++it) {
+          const int buf = it & 1;
+          const bool there = lane < tokens;
+          const bool wide = check_meta(km, ngk, (float)((1 << KB) - 1), there), big = bar_any(3, 256, wide);
+          if (big) scale_meta(km, ngk);
+          if (it >= 2) wait_warp(bKE + 8 * buf, ((it >> 1) - 1) & 1);
+          if (warp == 8 && lane == 0) sBig[it & 3] = big;
           uint8_t* dst = smem + sl.k + buf * T::kK;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int u = pass_token(k), n = 32 * blk + place_of(u);
-            uint8_t* row = dst + (n >> 3) * 128 + (n & 7) * 16;
-            uint32_t meta = __shfl_sync(FULL, km[0], u);
+          for (int k = 0; k < 2; ++k) {
+            const int u = token_at(8 * k + 16 * half + tl);
+            uint8_t* row = dst + (4 * blk + 2 * half + k) * 128 + tl * 16;
+            __half2 s, z;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
-              if (i > 0 && ((32 * i) & (g.gk - 1)) == 0) {       // a new group (the same for all lanes); group (32 i) / gk
+              if (i == 0 || ((32 * i) & (g.gk - 1)) == 0) {      // a new group (the same for all lanes)
                 const int e = (32 * i) / g.gk;
-                meta = __shfl_sync(FULL, e == 1 ? km[1 % NI] : e == 2 ? km[2 % NI] : km[3 % NI], u);
+                const uint32_t meta = __shfl_sync(FULL, e == 0 ? km[0] : e == 1 ? km[1 % NI] : e == 2 ? km[2 % NI] : km[3 % NI], u);
+                s = __low2half2(as_h2(meta)); z = __high2half2(as_h2(meta));
               }
-              const __half2 s = __low2half2(as_h2(meta)), z = __high2half2(as_h2(meta));
-              const uint32_t c0 = key_slot<KB, KW>(kw[k], 2 * i), c1_ = key_slot<KB, KW>(kw[k], 2 * i + 1);
-              *reinterpret_cast<uint4*>(row + (4 * i + ch) * T::kLbK) =
-                  make_uint4(values2(c0, 0x4140u, s, z), values2(c0, 0x4342u, s, z), values2(c1_, 0x4140u, s, z), values2(c1_, 0x4342u, s, z));
+              // slots 2 i and 2 i + 1: fields of a word, or words
+              constexpr int FPK = 8 / KB;
+              const uint32_t w0 = kw[k][(2 * i) / FPK], w1 = kw[k][(2 * i + 1) / FPK];
+              const int f0 = (2 * i) % FPK, f1 = (2 * i + 1) % FPK;
+              *reinterpret_cast<uint4*>(row + (4 * i + ch) * T::kLbK) = make_uint4(kc.values(w0, f0, s, z), kc.values(w0 >> 8, f0, s, z),
+                                                                                   kc.values(w1, f1, s, z), kc.values(w1 >> 8, f1, s, z));
             }
           }
-        }
-        tc::fence_async_smem();
-        __syncwarp();
-        if (lane == 0 && x + j != skip_x) mbar_arrive(bKF + 8 * buf);      // (skip_x: test hook - a page that never arrives)
-        step();
-        if (nx < x_hi) load_keys();
-        if (it >= 2) wait_warp(bVE + 8 * buf, ((it >> 1) - 1) & 1);
-        {
-          const int vl = lane >> 2, tq = lane & 3;   // channel of eight, place of the chunk
-          uint8_t* dst = smem + sl.v + buf * T::kV + vl * 16 + (4 * blk + tq) * T::kLbV;
+          tc::fence_async_smem();
+          __syncwarp();
+          if (lane == 0 && !(it == skip_it)) mbar_arrive(bKF + 8 * buf);
+          more = nc.on;
+          if (more) { to_next(); load(); }
+      }
+    } else {
+      // ------------------------------------------------------------ values: one of the octets of every sixteen channels
+      const int vl = lane & 7, tq = lane >> 3;       // channel of eight, place of the chunk
+      uint32_t vm[4] = {0u, 0u, 0u, 0u};
+      uint2 vw[NMW];
+      const Codes<VB> vc;
+      auto load = [&]() {
+        const uint8_t* v = page_ptr + g.v_codes_off + blk * (4 * D * VB) + (4 * vl + tq) * 16 + 8 * half;
+#pragma unroll
+        for (int mw = 0; mw < NMW; ++mw) vw[mw] = *reinterpret_cast<const uint2*>(v + 512 * mw);
+        load_meta(vm, g.v_meta_off, ngv);
+      };
+      bool more = nc.on;
+      if (more) { to_next(); load(); }
+#pragma unroll 1
+      for (; more; ++it) {
+          const int buf = it & 1;
+          const bool there = lane < tokens;
+          const bool wide = check_meta(vm, ngv, (float)((1 << VB) - 1), there);
+          const bool big = bar_any(4, 256, wide);
+          if (big) scale_meta(vm, ngv);
+          if (it >= 2) wait_warp(bVE + 8 * buf, ((it >> 1) - 1) & 1);
+          if (warp == 16 && lane == 0) sBig[4 + (it & 3)] = big;
+          uint8_t* dst = smem + sl.v + buf * T::kV + vl * 16 + (4 * blk + tq) * T::kLbV + 128 * half;
           __half2 s[2][2], z[2][2];                  // [half][pair of tokens]
 #pragma unroll
           for (int mw = 0; mw < NMW; ++mw) {
-            const uint32_t ww[4] = {vw[mw].x, vw[mw].y, vw[mw].z, vw[mw].w};
 #pragma unroll
             for (int f = 0; f < FPB; ++f) {
               const int m16 = mw * FPB + f;          // channels 16 m16 .. 16 m16 + 15
@@ -662,95 +748,99 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
                 for (int kh = 0; kh < 2; ++kh) {
 #pragma unroll
                   for (int pr = 0; pr < 2; ++pr) {
-                    const uint32_t m0 = __shfl_sync(FULL, own, 16 * kh + 2 * tq + pr), m1 = __shfl_sync(FULL, own, 16 * kh + 2 * tq + pr + 8);
+                    const uint32_t m0 = __shfl_sync(FULL, own, 16 * kh + 2 * tq + 8 * pr), m1 = __shfl_sync(FULL, own, 16 * kh + 2 * tq + 8 * pr + 1);
                     s[kh][pr] = as_h2(permute(m0, m1, 0x5410u));
                     z[kh][pr] = as_h2(permute(m0, m1, 0x7632u));
                   }
                 }
               }
-#pragma unroll
-              for (int rh = 0; rh < 2; ++rh) {
-                constexpr uint32_t M = ((1u << VB) - 1u) * 0x01010101u;
-                const uint32_t c0 = (ww[2 * rh] >> (VB * f)) & M, c1_ = (ww[2 * rh + 1] >> (VB * f)) & M;
-                *reinterpret_cast<uint4*>(dst + (2 * m16 + rh) * 128) =
-                    make_uint4(values2(c0, 0x4140u, s[0][0], z[0][0]), values2(c0, 0x4342u, s[0][1], z[0][1]),
-                               values2(c1_, 0x4140u, s[1][0], z[1][0]), values2(c1_, 0x4342u, s[1][1], z[1][1]));
-              }
+              // the octet's words of the two token halves: bytes 0, 2 are tokens 2 tq, 2 tq + 1 of the half, bytes 1, 3 those eight further
+              *reinterpret_cast<uint4*>(dst + 2 * m16 * 128) = make_uint4(vc.values(vw[mw].x, f, s[0][0], z[0][0]), vc.values(vw[mw].x >> 8, f, s[0][1], z[0][1]),
+                                                                          vc.values(vw[mw].y, f, s[1][0], z[1][0]), vc.values(vw[mw].y >> 8, f, s[1][1], z[1][1]));
             }
           }
-        }
-        tc::fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bVF + 8 * buf);
-        if (nx < x_hi) load_values();
+          tc::fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bVF + 8 * buf);
+          more = nc.on;
+          if (more) { to_next(); load(); }
       }
-    });
-  } else if (lane == 0) {
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
+    if (warp == 24) {
     // =========================================================== products
-    const uint32_t sk = smem_u32(smem + sl.k), sv = smem_u32(smem + sl.v), sqa = smem_u32(smem + sl.q);
-    bool ok = true;
-    auto wait = [&](uint32_t b, uint32_t parity) {
-      if (ok && !tc::wait_or_abort(b, parity, wait_ns, abort_flag)) {
-        ok = false;
-        *abort_flag = 1;
-        atomicOr(p.status, KVQ_STATUS_DEVICE_TIMEOUT);
-      }
-      return ok;
-    };
+    // The whole warp goes along on values that it shares (counts come from one lane), so that descriptors are made on the uniform path: a
+    // product per 64 cycles leaves the one thread that issues it few instructions.
+    const uint32_t dk = desc_low(smem_u32(smem + sl.k), T::kLbK), dv = desc_low(smem_u32(smem + sl.v), T::kLbV), dq = desc_low(smem_u32(smem + sl.q), T::kLbQ);
+    const uint32_t tm = __shfl_sync(FULL, tmem, 0);
     auto keys = [&](int w, int buf) {                // S = Q K^T
+      const uint32_t a = dq + w * (T::kQ >> 4), b = dk + buf * (T::kK >> 4), d = tm + kColS + 128 * w;
+      if (elect_one()) {
+        mma_ss<false>(d, a, b, idesc(128));
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k)
-        mma_ss(tmem + kColS + 128 * w, smem_desc(sqa + w * T::kQ + 2 * k * T::kLbQ, T::kLbQ, 128), smem_desc(sk + buf * T::kK + 2 * k * T::kLbK, T::kLbK, 128),
-               idesc(128), k > 0);
-      tc::tc_commit(bS + 8 * w);
-    };
-    auto values = [&](int w, int buf, bool fresh) {  // O += P V
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        mma_ts(tmem + kColO + 128 * w, tmem + kColS + 128 * w + 8 * k, smem_desc(sv + buf * T::kV + 2 * k * T::kLbV, T::kLbV, 128), idesc(D), k > 0 || !fresh);
-    };
-    int it = 0, done[2] = {0, 0}, seg[2] = {0, 0};
-    segments([&](const Tile& t, int page0, int pages, long long x) {
-      const int halves = t.i * kTile + 128 < t.pairs ? 2 : 1;
-      // the first page's S of both halves
-      for (int w = 0; w < halves && ok; ++w) {
-        if (!wait(bQ + 8 * w, seg[w] & 1)) break;
-        ++seg[w];
-        if (w == 0 && !wait(bKF + 8 * (it & 1), (it >> 1) & 1)) break;
-        tc::tc_fence_after();
-        keys(w, it & 1);
+        for (int k = 1; k < D / 16; ++k) mma_ss<true>(d, a + k * (2 * T::kLbQ >> 4), b + k * (2 * T::kLbK >> 4), idesc(128));
+        tc::tc_commit(bS + 8 * w);
       }
-      if (ok) tc::tc_commit(bKE + 8 * (it & 1));
-      // then, page by page and half by half: O of this page, S of the next
-      for (int j = 0; j < pages && ok; ++j, ++it) {
-        const int buf = it & 1, nbuf = buf ^ 1;
-        if (!wait(bVF + 8 * buf, (it >> 1) & 1)) break;
-        for (int w = 0; w < halves && ok; ++w) {
-          if (!wait(bP + 8 * w, done[w] & 1)) break;
-          ++done[w];
-          tc::tc_fence_after();
-          values(w, buf, j == 0);
-          if (w == halves - 1) tc::tc_commit(bVE + 8 * buf);
-          if (j + 1 < pages) {
-            if (w == 0 && !wait(bKF + 8 * nbuf, ((it + 1) >> 1) & 1)) break;
+      __syncwarp();
+    };
+    auto values = [&](int w, int buf, uint32_t add) {  // O += P V
+      const uint32_t a = tm + kColS + 128 * w, b = dv + buf * (T::kV >> 4), d = tm + kColO + 128 * w;
+      if (elect_one()) {
+        mma_ts(d, a, b, idesc(D), add);
+#pragma unroll
+        for (int k = 1; k < 8; ++k) mma_ts(d, a + 8 * k, b + k * (2 * T::kLbV >> 4), idesc(D), 1u);
+      }
+      __syncwarp();
+    };
+    auto commit = [&](uint32_t b) {
+      if (elect_one()) tc::tc_commit(b);
+      __syncwarp();
+    };
+    uint32_t it = 0, done = 0, seg = 0;              // pages; phases of P (page 2^w) and of the queries, a bit per half
+#pragma unroll 1
+    for (Cursor c = start(); c.on; advance(c)) {
+      const int halves = __shfl_sync(FULL, c.t.i * kTile + 128 < c.t.pairs ? 2 : 1, 0), pages = __shfl_sync(FULL, c.end - c.page, 0);
+      // step 0: the first page's S of both halves; then, page by page and half by half: O of this page, S of the next
+#pragma unroll 1
+      for (int j = -1; j < pages; ++j) {
+        const uint32_t buf = it & 1, nbuf = (it + (j >= 0)) & 1;
+        if (j >= 0) wait_warp(bVF + 8 * buf, (it >> 1) & 1);
+#pragma unroll 1
+        for (int w = 0; w < halves; ++w) {
+          if (j >= 0) {
+            wait_warp(bP + 8 * w, (done >> w) & 1);
+            done ^= 1u << w;
             tc::tc_fence_after();
-            keys(w, nbuf);
-            if (w == halves - 1) tc::tc_commit(bKE + 8 * nbuf);
+            if (!aborted) values(w, buf, j > 0);
+            if (w == halves - 1) commit(bVE + 8 * buf);
           } else {
-            tc::tc_commit(bO + 8 * w);
+            wait_warp(bQ + 8 * w, (seg >> w) & 1);
+            seg ^= 1u << w;
+          }
+          if (j + 1 < pages) {
+            if (w == 0) wait_warp(bKF + 8 * nbuf, ((it + (j >= 0)) >> 1) & 1);
+            tc::tc_fence_after();
+            if (!aborted) keys(w, nbuf);
+            if (w == halves - 1) commit(bKE + 8 * nbuf);
+          } else {
+            commit(bO + 8 * w);
           }
         }
+        if (j >= 0) ++it;
       }
-    });
+    }
     // nothing of this CTA's may still run on the tensor cores when its tensor memory is freed
-    tc::tc_commit(bDrain);
-    mbar_wait(bDrain, 0, wait_ns);
+    commit(bDrain);
+    if (lane == 0) mbar_wait(bDrain, 0, wait_ns);
+    __syncwarp();
+    }
   }
   __syncwarp();
   tc::tc_fence_before();
   __syncthreads();
   tc::tc_fence_after();
-  if (warp == 12) tc::tmem_dealloc(tmem, kTmemCols);
+  if (warp == 24) tc::tmem_dealloc(tmem, kTmemCols);
 }
 
 template <int D, int KB, int VB>
@@ -758,6 +848,12 @@ int launch_chunk_inst(const Geom& g, const Paged& p, const void* q, float c1, fl
                       unsigned long long wait_ns, long long skip_x, cudaStream_t stream) {
   const Smem sl = smem_of<D>(g.B);
   auto kern = chunk_kernel<D, KB, VB>;
+  // (an increase of registers waits for ever where the block was launched with fewer than the roles take together)
+  static const bool fits = [&] {
+    cudaFuncAttributes a;
+    return cudaFuncGetAttributes(&a, kern) == cudaSuccess && a.numRegs >= kRegsLaunch;
+  }();
+  if (!fits) return KVQ_ERR_CUDA_LAUNCH;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, sl.total) != cudaSuccess) return KVQ_ERR_CUDA_LAUNCH;
   const long long pairs = (long long)p.max_rows * g.G;
   const cudaError_t e = launch_dependent(kern, dim3(kGrid), kThreads, sl.total, stream, 1, g, p, static_cast<const uint16_t*>(q), c1, ws,
