@@ -74,10 +74,10 @@ __device__ __forceinline__ void rotate_row(float (&x)[8], const RopeArgs& r, con
 }
 
 // Rows of a token: n_kv_heads keys, as many values where V_ROWS, then the query heads.  A warp takes 256 / D of them at a time and
-// `groups` such in a row, the next one's loads in flight: the token's angles stay in registers.
+// `groups` such in a row, the next two's loads in flight: the token's angles stay in registers.
 // Long calls are bound by the memory system (8B shape, 32,768 tokens: see launch_paged_append), single tokens by latency.
 template <int D, int DTYPE, bool V_ROWS>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 paged_append_rows_kernel(Geom g, Paged p, AppendArgs a, int per_token, int groups) {
   constexpr int LPR = D / 8, RPW = 32 / LPR;
   const int lane = threadIdx.x & 31, l = lane % LPR;
@@ -102,7 +102,8 @@ paged_append_rows_kernel(Geom g, Paged p, AppendArgs a, int per_token, int group
     src += s.is_k || s.is_v ? (long long)row * a.kv_row + (long long)s.head * a.kv_head : (long long)row * a.q_row + (long long)s.head * a.q_head;
     return s.on ? __ldcs(reinterpret_cast<const uint4*>(src + 8 * l)) : make_uint4(0u, 0u, 0u, 0u);
   };
-  uint4 next = fetch(g0);                        // (on its way while the sequence is looked up; rows of padding exist too)
+  // (on their way while the sequence is looked up; rows of padding exist too)
+  uint4 next = fetch(g0), after = g0 + 1 < g1 ? fetch(g0 + 1) : make_uint4(0u, 0u, 0u, 0u);
   const int b = sequence_of(p.cu, g.B, row, lane);
   bool bad;
   const int limit = a.rope.half ? min(g.capacity, a.rope.n_positions) : g.capacity;
@@ -120,7 +121,8 @@ paged_append_rows_kernel(Geom g, Paged p, AppendArgs a, int per_token, int group
   const bool active = sl.on, is_k = sl.is_k, is_v = sl.is_v;
   const int head = sl.head;
   const uint4 raw = next;
-  if (group + 1 < g1) next = fetch(group + 1);
+  next = after;
+  if (group + 2 < g1) after = fetch(group + 2);
   float x[8];
   unpack8<DTYPE>(raw, x);
   if (a.rope.half) {

@@ -567,49 +567,67 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       if (const_cast<volatile int*>(sMisc)[2 + w] == parts) {
         __threadfence();
         const int rows_w = min(128, t.pairs - pair0);
-        for (int idx = row; idx < rows_w * (D / 4); idx += 128) {
-          const int rr = idx / (D / 4), c4 = idx % (D / 4), pr = pair0 + rr;
-          float ms = -INFINITY, den = 0.f;
-          float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float2* mls = reinterpret_cast<const float2*>(ws + ml_offset_floats(cap, D));
+        // the parts' places: the tile starts in the second one of its first CTA, goes on in the first one of those behind
+        auto place = [&](int j) { return (size_t)(2 * (first + j) + (j == 0 ? 1 : 0)) * cap + 128 * w; };
+        // a thread per 16 bytes of a row, two rows of four parts in flight at a time
+        constexpr int NP = D / 4, U = 2;
 #pragma unroll 1
-          for (int j0 = 0; j0 < parts; j0 += 8) {
-            float2 ml[8];
-            float4 o[8];
+        for (int idx0 = row; idx0 < rows_w * NP; idx0 += 128 * U) {
+          float4 num[U];
+          float ms[U], den[U];
+          int rr[U];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              const int j = min(j0 + u, parts - 1);
-              const size_t at = (size_t)(2 * (first + j) + (j == 0 ? 1 : 0)) * cap + 128 * w + rr;
-              ml[u] = __ldcg(reinterpret_cast<const float2*>(ws + ml_offset_floats(cap, D)) + at);
-              o[u] = __ldcg(reinterpret_cast<const float4*>(ws + at * D) + c4);
-              if (j0 + u >= parts) ml[u].x = -INFINITY;
-            }
-            float mb = ms;
+          for (int u = 0; u < U; ++u) {
+            rr[u] = min(idx0 + 128 * u, rows_w * NP - 1) / NP;
+            ms[u] = -INFINITY;
+            den[u] = 0.f;
+            num[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+#pragma unroll 1
+          for (int j = 0; j < parts; j += 4) {
+            float2 ml[4][U];
+            float4 o[4][U];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) mb = fmaxf(mb, ml[u].x);
-            if (mb == -INFINITY) continue;
-            const float keep = ms == -INFINITY ? 0.f : ex2(ms - mb);
-            den *= keep; num.x *= keep; num.y *= keep; num.z *= keep; num.w *= keep;
+            for (int e = 0; e < 4; ++e) {
+              const size_t at = place(min(j + e, parts - 1));
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              const float wt = ml[u].x == -INFINITY ? 0.f : ex2(ml[u].x - mb);
-              if (wt != 0.f) {
-                den = fmaf(wt, ml[u].y, den);
-                num.x = fmaf(wt, o[u].x, num.x); num.y = fmaf(wt, o[u].y, num.y);
-                num.z = fmaf(wt, o[u].z, num.z); num.w = fmaf(wt, o[u].w, num.w);
+              for (int u = 0; u < U; ++u) {
+                ml[e][u] = __ldcg(mls + at + rr[u]);
+                o[e][u] = __ldcg(reinterpret_cast<const float4*>(ws + (at + rr[u]) * D) + (idx0 & (NP - 1)));
+                if (j + e >= parts) ml[e][u].x = -INFINITY;
               }
             }
-            ms = mb;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const float mb = fmaxf(ms[u], fmaxf(fmaxf(ml[0][u].x, ml[1][u].x), fmaxf(ml[2][u].x, ml[3][u].x)));
+              if (mb == -INFINITY) continue;         // (a part without a token for this row: its o is zero, its sum too)
+              const float w0 = ms[u] == -INFINITY ? 0.f : ex2(ms[u] - mb);
+              den[u] *= w0; num[u].x *= w0; num[u].y *= w0; num[u].z *= w0; num[u].w *= w0;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float wt = ml[e][u].x == -INFINITY ? 0.f : ex2(ml[e][u].x - mb);
+                den[u] = fmaf(wt, ml[e][u].y, den[u]);
+                num[u].x = fmaf(wt, o[e][u].x, num[u].x); num[u].y = fmaf(wt, o[e][u].y, num[u].y);
+                num[u].z = fmaf(wt, o[e][u].z, num[u].z); num[u].w = fmaf(wt, o[e][u].w, num[u].w);
+              }
+              ms[u] = mb;
+            }
           }
-          const float iv = den > 0.f ? 1.0f / den : 0.f;
-          const int rw = by_g(pr);
-          const size_t at = ((size_t)(t.first + rw) * g.Hq + (size_t)t.h * G + (pr - rw * G)) * D + 4 * c4;
-          if (out_dtype == KVQ_FP32) {
-            *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(num.x * iv, num.y * iv, num.z * iv, num.w * iv);
-          } else {
-            uint2 v;
-            v.x = (uint32_t)f32_to_bits16(num.x * iv, out_dtype) | ((uint32_t)f32_to_bits16(num.y * iv, out_dtype) << 16);
-            v.y = (uint32_t)f32_to_bits16(num.z * iv, out_dtype) | ((uint32_t)f32_to_bits16(num.w * iv, out_dtype) << 16);
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = v;
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            if (idx0 + 128 * u >= rows_w * NP) break;
+            const float iv = den[u] > 0.f ? 1.0f / den[u] : 0.f;
+            const int rw = by_g(pair0 + rr[u]);
+            const size_t at = ((size_t)(t.first + rw) * g.Hq + (size_t)t.h * G + (pair0 + rr[u] - rw * G)) * D + 4 * (idx0 & (NP - 1));
+            if (out_dtype == KVQ_FP32) {
+              *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(num[u].x * iv, num[u].y * iv, num[u].z * iv, num[u].w * iv);
+            } else {
+              uint2 v;
+              v.x = (uint32_t)f32_to_bits16(num[u].x * iv, out_dtype) | ((uint32_t)f32_to_bits16(num[u].y * iv, out_dtype) << 16);
+              v.y = (uint32_t)f32_to_bits16(num[u].z * iv, out_dtype) | ((uint32_t)f32_to_bits16(num[u].w * iv, out_dtype) << 16);
+              *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = v;
+            }
           }
         }
         if (row == 0) counts[2 * first + w] = 0ull;

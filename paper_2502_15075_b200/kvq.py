@@ -441,7 +441,9 @@ class PagedCache:
         assert pages.device == block_table.device == seq_len.device
         self.pages, self.block_table, self.seq_len = pages, block_table, seq_len
         self.status = torch.zeros(1, dtype=torch.int32, device=pages.device)
+        self.device_index = pages.get_device()
         stride = block_table.stride(0) if cfg.batch > 1 else max(columns, block_table.stride(0))
+        # (a call costs the host about as much as a small kernel the GPU: nothing is made twice that can be kept)
         self.c = kvq_paged_cache(pages.data_ptr(), pages.shape[0], block_table.data_ptr(), stride, seq_len.data_ptr(), self.status.data_ptr())
 
 
@@ -451,20 +453,25 @@ class Rope:
     def __init__(self, cos: torch.Tensor, sin: torch.Tensor, interleaved: bool = False):
         assert cos.is_cuda and cos.device == sin.device and cos.dim() == 2 and cos.shape == sin.shape
         assert cos.dtype == torch.float32 and sin.dtype == torch.float32 and cos.is_contiguous() and sin.is_contiguous()
-        self.cos, self.sin = cos, sin
+        self.cos, self.sin, self.device_index = cos, sin, cos.get_device()
         self.c = kvq_rope(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)))
 
 
+def _device_reader(c=torch._C):
+    """How the current device's number is read: torch's (private) call where it has it, which costs a tenth of the public one."""
+    return getattr(c, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+_current_device = _device_reader()
+
+
 def _ragged(cfg: kvq_config, cache: PagedCache, cu: torch.Tensor, *tensors: torch.Tensor):
-    """The checks that all paged calls share: the offsets, and everything on the pool's device."""
-    assert cu.dtype == torch.int32 and cu.dim() == 1 and cu.shape[0] == cfg.batch + 1 and cu.is_contiguous()
-    device = cache.pages.device
-    assert cu.device == device and all(t.device == device for t in tensors), "all tensors on the pool's device"
-
-
-def _on_device(cache: PagedCache):
-    """The library launches on the current device: it has to be the pool's."""
-    assert cache.pages.device.index == torch.cuda.current_device(), "the pool's device has to be the current one (torch.cuda.device)"
+    """The checks that all paged calls share: the offsets, and everything on the pool's device, which is the one that is launched on."""
+    assert cu.dtype is torch.int32 and cu.shape == (cfg.batch + 1,) and cu.is_contiguous()
+    device = cache.device_index
+    assert cu.get_device() == device and _current_device() == device, "the pool's device has to be the current one (torch.cuda.device)"
+    for t in tensors:
+        assert t.get_device() == device, "all tensors on the pool's device"
 
 
 def kvq_paged_append(cfg: kvq_config, cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor,
@@ -472,21 +479,22 @@ def kvq_paged_append(cfg: kvq_config, cache: PagedCache, k: torch.Tensor, v: tor
                      stream: Optional[torch.cuda.Stream] = None):
     """k, v [rows, Hkv, D] of the config's dtype with identical strides (e.g. slices of one projection output), last dim contiguous;
     cu int32 [batch + 1].  rope: rotate k (and q, to q_out [rows, Hq, D] contiguous) by position first."""
-    n = k.shape[0]
-    strides = k.stride()
-    assert k.dim() == 3 and k.shape == v.shape and strides == v.stride() and strides[2] == 1
-    assert k.shape[1] == cfg.n_kv_heads and k.shape[2] == cfg.head_dim and v.dtype == k.dtype and _dtype_code(k.dtype) == cfg.in_dtype
+    shape, strides, dtype = k.shape, k.stride(), k.dtype
+    n, heads, dim = shape
+    assert heads == cfg.n_kv_heads and dim == cfg.head_dim and shape == v.shape and strides == v.stride() and strides[2] == 1
+    assert v.dtype is dtype and _DTYPE_CODES[dtype] == cfg.in_dtype
     _ragged(cfg, cache, cu, k, v)
-    _on_device(cache)
     q_ptr = out_ptr = None
     q_strides = (0, 0)
     assert (q is None) == (q_out is None), "q and q_out together"
     if q is not None:
-        assert q.dim() == 3 and q.shape == (n, cfg.n_q_heads, cfg.head_dim) and q.stride(2) == 1 and q.dtype == k.dtype
-        assert q_out.shape == q.shape and q_out.is_contiguous() and q_out.dtype == q.dtype and q.device == q_out.device == k.device
-        q_ptr, out_ptr, q_strides = q.data_ptr(), q_out.data_ptr(), q.stride()
+        q_shape, q_strides = q.shape, q.stride()
+        assert q_shape == (n, cfg.n_q_heads, dim) and q_strides[2] == 1 and q.dtype is dtype
+        assert q_out.shape == q_shape and q_out.is_contiguous() and q_out.dtype is dtype
+        assert q.get_device() == q_out.get_device() == cache.device_index
+        q_ptr, out_ptr = q.data_ptr(), q_out.data_ptr()
     if rope is not None:
-        assert rope.cos.device == k.device
+        assert rope.device_index == cache.device_index
     _check(_lib.kvq_paged_append(ctypes.byref(cfg), ctypes.byref(cache.c), k.data_ptr(), v.data_ptr(), strides[0], strides[1],
                                  cu.data_ptr(), n, None if rope is None else ctypes.byref(rope.c), q_ptr, q_strides[0], q_strides[1],
                                  out_ptr, _stream_ptr(stream)), "kvq_paged_append")
@@ -504,13 +512,14 @@ def kvq_paged_attention(cfg: kvq_config, cache: PagedCache, q: torch.Tensor, cu:
     """q, out [rows, Hq, D] contiguous (q of the config's dtype, out fp16/bf16/fp32); cu int32 [batch + 1]; no sequence has more
     than max_rows rows; workspace: uint8 CUDA tensor of at least kvq_paged_workspace_bytes(cfg, max_rows).  A row at position p sees the
     tokens t <= p with t > p - window or t < sinks (window 0: all of them)."""
-    assert q.dim() == 3 and q.shape[1] == cfg.n_q_heads and q.shape[2] == cfg.head_dim and out.shape == q.shape
-    assert q.is_contiguous() and out.is_contiguous() and workspace.is_contiguous() and _dtype_code(q.dtype) == cfg.in_dtype
+    shape = q.shape
+    n, heads, dim = shape
+    assert heads == cfg.n_q_heads and dim == cfg.head_dim and out.shape == shape
+    assert q.is_contiguous() and out.is_contiguous() and workspace.is_contiguous() and _DTYPE_CODES[q.dtype] == cfg.in_dtype
     _ragged(cfg, cache, cu, q, out, workspace)
-    _on_device(cache)
-    _check(_lib.kvq_paged_attention(ctypes.byref(cfg), ctypes.byref(cache.c), q.data_ptr(), cu.data_ptr(), q.shape[0], int(max_rows),
-                                    int(window), int(sinks), out.data_ptr(), _dtype_code(out.dtype), float(softmax_scale),
-                                    workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+    _check(_lib.kvq_paged_attention(ctypes.byref(cfg), ctypes.byref(cache.c), q.data_ptr(), cu.data_ptr(), n, max_rows,
+                                    window, sinks, out.data_ptr(), _DTYPE_CODES[out.dtype], softmax_scale,
+                                    workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)),
            "kvq_paged_attention")
 
 
@@ -528,11 +537,10 @@ def kvq_paged_dequantize(cfg: kvq_config, cache: PagedCache, cu: torch.Tensor, k
     """k_out, v_out [rows, Hkv, D] contiguous of the config's dtype (or None): the tokens of the call's rows in 16 bits."""
     given = [t for t in (k_out, v_out) if t is not None]
     _ragged(cfg, cache, cu, *given)
-    _on_device(cache)
+    n = given[0].shape[0] if given else 0
     for t in given:
-        assert t.dim() == 3 and t.is_contiguous() and _dtype_code(t.dtype) == cfg.in_dtype
-        assert t.shape[0] == given[0].shape[0] and tuple(t.shape[1:]) == (cfg.n_kv_heads, cfg.head_dim)
-    _check(_lib.kvq_paged_dequantize(ctypes.byref(cfg), ctypes.byref(cache.c), cu.data_ptr(), given[0].shape[0] if given else 0,
+        assert t.shape == (n, cfg.n_kv_heads, cfg.head_dim) and t.is_contiguous() and _DTYPE_CODES[t.dtype] == cfg.in_dtype
+    _check(_lib.kvq_paged_dequantize(ctypes.byref(cfg), ctypes.byref(cache.c), cu.data_ptr(), n,
                                      k_out.data_ptr() if k_out is not None else None,
                                      v_out.data_ptr() if v_out is not None else None, _stream_ptr(stream)), "kvq_paged_dequantize")
 
