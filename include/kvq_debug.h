@@ -68,7 +68,7 @@ int kvq_debug_divide(const int64_t* n, const int64_t* d, int64_t* q, int32_t cou
 
 /* kvq_paged_attention with every device-side wait limited to wait_us microseconds (1 .. 100000) and one page withheld: the flat page
  * skip_page (counted over all (sequence, KV head) streams' seen pages, as in kvq_debug_decode_stall) of the decode kernel, page
- * skip_page % 256 of those of CTA skip_page / 256 of the chunk kernel; -1: none.  As there the call ends, sets KVQ_STATUS_DEVICE_TIMEOUT and
+ * skip_page (from 0) of every CTA's share of the chunk kernel; -1: none.  As there the call ends, sets KVQ_STATUS_DEVICE_TIMEOUT and
  * leaves the workspace usable. */
 int kvq_debug_paged_stall(const kvq_config* cfg, const kvq_paged_cache* cache, const void* q, const int32_t* cu, int32_t n_rows,
                           int32_t max_rows, int32_t window, int32_t sinks, void* out, int32_t out_dtype, void* workspace,

@@ -3,13 +3,13 @@
 //
 // A tile is 256 (query row, head) pairs of one sequence and KV head - the query heads of a KV head are rows of one product - against pages of 128
 // tokens.  One CTA per SM:
-//  * warps 8-15 (keys) and 16-23 (values) turn a page into 16-bit tiles in shared memory: codes become fp16 by a mask under the bits of 1024 and
+//  * warps 16-23 (keys) and 24-27 (values) turn a page into 16-bit tiles in shared memory: codes become fp16 by a mask under the bits of 1024 and
 //    an exact operation, scale and zero-point enter by a fused one (one rounding, 2^-11 of the value at most).  Their packed words were
 //    loaded a page ahead, straight into registers.  The order of channels (keys) and of tokens (both) is the one in which codes lie in the
 //    page; queries and the weights follow it, so that nothing is transposed.
-//  * one thread of warp 24 issues tcgen05.mma (kind f16, M 128, fp32 accumulators in tensor memory): S = Q K^T of both halves of the tile
+//  * one thread of warp 28 issues tcgen05.mma (kind f16, M 128, fp32 accumulators in tensor memory): S = Q K^T of both halves of the tile
 //    in turn, and O += P V with P read from tensor memory, where it takes the place of S.
-//  * warps 0-3 and 4-7 take the two halves, a thread per row: row maximum, p = 2^(x - reference), fp16 weights back to tensor memory;
+//  * warps 0-7 and 8-15 take the two halves, two threads per row: row maximum, p = 2^(x - reference), fp16 weights back to tensor memory;
 //    sums in fp32.  While one half's softmax runs, the tensor cores have the other half's products.  The reference moves only when a logit
 //    passes it by kHeadroom bits; then the row's outputs are rescaled in tensor memory.
 // The order of the fp16 weights' rounding (2^-11 of a weight at most) and of the tiles' is the loss against fp32; all sums are fp32.
@@ -30,17 +30,17 @@ namespace chunk {
 
 using namespace mma;
 
-constexpr int kThreads = 28 * 32;          // warps 0-7 softmax, 8-15 keys, 16-23 values, 24 products (25-27 complete its warpgroup)
-// Registers per thread at launch, and of the roles: 256 softmax threads, 512 that make tiles, 128 more.
-constexpr int kRegsLaunch = 72, kRegsSoftmax = 104, kRegsTiles = 56, kRegsRest = 72;
-static_assert(256 * kRegsSoftmax + 512 * kRegsTiles + 128 * kRegsRest <= kThreads * kRegsLaunch, "an increase waits for registers that the others gave up");
+constexpr int kThreads = 32 * 32;          // warps 0-15 softmax, 16-23 keys, 24-27 values, 28 products (29-31 complete its warpgroup)
+// Registers per thread at launch, and of the roles: 512 softmax threads, 384 that make tiles, 128 more.
+constexpr int kRegsLaunch = 64, kRegsSoftmax = 80, kRegsTiles = 48, kRegsRest = 48;
+static_assert(512 * kRegsSoftmax + 384 * kRegsTiles + 128 * kRegsRest <= kThreads * kRegsLaunch, "an increase waits for registers that the others gave up");
 constexpr int kGrid = 148;
 constexpr int kTile = 256;                 // (query row, head) pairs of a tile
-constexpr int kGap = 2;                    // what a tile costs besides its pages (queries, a first product that nothing overlaps, outputs), in pages
+constexpr int kGap = 5;                    // what a tile costs besides its pages (queries, a first product that nothing overlaps, outputs), in pages
 constexpr float kHeadroom = 4.0f;
 constexpr float kBigDown = 9.765625e-4f, kBigUp = 1024.0f;      // 2^-10 for pages whose values pass half the fp16 range, and back
 constexpr uint32_t FULL = 0xffffffffu;
-// tensor memory: S of the two halves (their first 64 columns take P), then O of the two halves
+// tensor memory: S of the two halves (columns 0-31 and 64-95 of each take P), then O of the two halves
 constexpr uint32_t kColS = 0, kColO = 256, kTmemCols = 512;
 // fp16 operands, fp32 accumulate, both K-major, M 128
 __host__ __device__ constexpr uint32_t idesc(int n) { return (1u << 4) | ((uint32_t)(n / 8) << 17) | (8u << 24); }
@@ -51,7 +51,7 @@ template <int D> struct Tiles {
   static constexpr int kLbQ = 128 * 16, kLbK = 128 * 16, kLbV = D * 16;
   static constexpr int kQ = D / 8 * kLbQ, kK = D / 8 * kLbK, kV = 16 * kLbV;      // bytes of a query half, a key and a value tile
 };
-struct Smem { int q, k, v, bars, misc, pref, seq, total; };
+struct Smem { int q, k, v, bars, misc, rows, pref, seq, total; };
 template <int D>
 __host__ __device__ inline Smem smem_of(int batch) {
   using T = Tiles<D>;
@@ -61,7 +61,8 @@ __host__ __device__ inline Smem smem_of(int batch) {
   s.v = s.k + 2 * T::kK;
   s.bars = s.v + 2 * T::kV;
   s.misc = s.bars + 32 * 8;
-  s.pref = s.misc + 64;
+  s.rows = s.misc + 64;                      // per row of the tile: what its two threads tell each other, for two pages in turn
+  s.pref = s.rows + 2 * kTile * 2 * 4;
   s.seq = s.pref + (batch + 1) * 8;
   s.total = s.seq + 3 * batch * 4;
   return s;
@@ -97,26 +98,22 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint3
 #define KVQ_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
 #define KVQ_W8(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
 #define KVQ_S8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : KVQ_R8(r, 0), KVQ_R8(r, 8), KVQ_R8(r, 16), KVQ_R8(r, 24) : "r"(addr) : "memory");
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : KVQ_R8(r, 0), KVQ_R8(r, 8) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void wait_ld(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : KVQ_W8(r, 0), KVQ_W8(r, 8)::"memory");
 }
 // Waits for this thread's loads from tensor memory; the registers go through it, so that nothing is computed from them before.
-__device__ __forceinline__ void wait_ld(uint32_t (&r)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;" : KVQ_W8(r, 0), KVQ_W8(r, 8), KVQ_W8(r, 16), KVQ_W8(r, 24)::"memory");
-}
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-      ::"r"(addr), KVQ_S8(r, 0), KVQ_S8(r, 8), KVQ_S8(r, 16), KVQ_S8(r, 24) : "memory");
-}
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
       ::"r"(addr), KVQ_S8(r, 0), KVQ_S8(r, 8) : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr), KVQ_S8(r, 0) : "memory");
 }
 __device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t sel) {
   uint32_t d;
@@ -196,14 +193,14 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
   if (tid_ == 0) {
     sMisc[0] = 0;
     for (int k = 0; k < 2; ++k) {
-      mbar_init(bKF + 8 * k, 8); mbar_init(bKE + 8 * k, 1); mbar_init(bVF + 8 * k, 8); mbar_init(bVE + 8 * k, 1);
-      mbar_init(bQ + 8 * k, 4); mbar_init(bS + 8 * k, 1); mbar_init(bP + 8 * k, 4); mbar_init(bO + 8 * k, 1);
+      mbar_init(bKF + 8 * k, 8); mbar_init(bKE + 8 * k, 1); mbar_init(bVF + 8 * k, 4); mbar_init(bVE + 8 * k, 1);
+      mbar_init(bQ + 8 * k, 8); mbar_init(bS + 8 * k, 1); mbar_init(bP + 8 * k, 8); mbar_init(bO + 8 * k, 1);
     }
     mbar_init(bDrain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   begin_after_predecessor();
-  if (warp == 24) {
+  if (warp == 28) {
     tc::tmem_alloc(smem_u32(&sMisc[1]), kTmemCols);
     tc::tmem_relinquish();
   }
@@ -353,14 +350,26 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
     }
   };
 
-  if (warp < 8) {
+  if (warp < 16) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-    // =========================================================== softmax: half w of the tile, a thread per row
-    const int w = warp >> 2, row = tid_ & 127;
-    const uint32_t tS = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColS + 128 * w, tO = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColO + 128 * w;
-    uint8_t* sq = smem + sl.q + w * T::kQ + (row >> 3) * 128 + (row & 7) * 16;
+    // =========================================================== softmax: half w of the tile, two threads per row, each with a side of 64 of the
+    // page's columns and half of the channels (one thread per row: the softmax's latency, which the products wait for, is half as long again)
+    const int w = warp >> 3, side = (warp >> 2) & 1, row = 32 * (warp & 3) + lane;
+    const uint32_t tS = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColS + 128 * w + 64 * side;
+    const uint32_t tO = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColO + 128 * w + D / 2 * side;
+    uint8_t* sq = smem + sl.q + w * T::kQ + row * 16 + side * (D / 16) * T::kLbQ;
+    volatile float* sRow = reinterpret_cast<float*>(smem + sl.rows) + (128 * w + row) * 2;      // [page parity][row][side]
     const unsigned long long id40 = (call_id & 0xFFFFFFFFFFull) ? (call_id & 0xFFFFFFFFFFull) : 1ull;
     unsigned long long* counts = reinterpret_cast<unsigned long long*>(ws + count_offset_floats(cap, D));
+    // a value for the row's other thread, and its
+    uint32_t turn = 0;
+    auto exchange = [&](float x) {
+      volatile float* at = sRow + turn * (2 * kTile);
+      turn ^= 1;
+      at[side] = x;
+      named_bar_sync(1 + w, 256);
+      return at[side ^ 1];
+    };
     int it = 0, done = 0, seg = 0;                   // pages of the share so far, those that this half had, segments it had
 #pragma unroll 1
     for (Cursor c = start(); c.on; advance(c)) {
@@ -374,29 +383,35 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       float f = c1;
       {
         const uint16_t* src = q + ((size_t)(t.first + r) * g.Hq + (size_t)t.h * G + (pair - r * G)) * D;
-        uint32_t qw[D / 2];                          // (the whole row at once: one wait for memory)
+        uint32_t qw[D / 4];                          // (this side's channels at once: one wait for memory)
 #pragma unroll
-        for (int k = 0; k < D / 8; ++k) {
+        for (int k = 0; k < D / 16; ++k) {
           uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (real) v = *reinterpret_cast<const uint4*>(src + 8 * k);
+          if (real) v = *reinterpret_cast<const uint4*>(src + side * (D / 2) + 8 * k);
           qw[4 * k] = v.x; qw[4 * k + 1] = v.y; qw[4 * k + 2] = v.z; qw[4 * k + 3] = v.w;
         }
         // |q| has the order of its 16-bit pattern: bf16 rows are scaled to bring the exponent of the largest to that of one
         if (g.in_dtype == KVQ_BF16) {
           uint32_t top = 0;
 #pragma unroll
-          for (int k = 0; k < D / 2; ++k) top = __vmaxu2(top, qw[k] & 0x7FFF7FFFu);
+          for (int k = 0; k < D / 4; ++k) top = __vmaxu2(top, qw[k] & 0x7FFF7FFFu);
+#pragma unroll 4
+          for (int k = 0; k < D / 16; ++k) {         // (the other side's)
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (real) v = *reinterpret_cast<const uint4*>(src + (side ^ 1) * (D / 2) + 8 * k);
+            top = __vmaxu2(__vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)), top);
+          }
           const int e = (int)(max(top & 0xFFFFu, top >> 16) >> 7);
           const int shift = e == 0 ? 0 : min(max(127 - e, -126), 126);
           const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
           f = c1 * __uint_as_float((uint32_t)(127 - shift) << 23);
 #pragma unroll
-          for (int k = 0; k < D / 2; ++k)
+          for (int k = 0; k < D / 4; ++k)
             qw[k] = as_u32(__floats2half2_rn(__uint_as_float(qw[k] << 16) * up, __uint_as_float(qw[k] & 0xFFFF0000u) * up));
         }
         // chunk 4 i + ch: channels 32 i + 4 ch + {0, 2, 1, 3}, then those 16 further
 #pragma unroll
-        for (int k = 0; k < D / 8; ++k) {
+        for (int k = 0; k < D / 16; ++k) {
           const int i = k >> 2, ch = k & 3, a = (32 * i + 4 * ch) / 2;
           *reinterpret_cast<uint4*>(sq + k * T::kLbQ) = make_uint4(permute(qw[a], qw[a + 1], 0x5410u), permute(qw[a], qw[a + 1], 0x7632u),
                                                                    permute(qw[a + 8], qw[a + 9], 0x5410u), permute(qw[a + 8], qw[a + 9], 0x7632u));
@@ -406,6 +421,11 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       tc::tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bQ + 8 * w);
+      // the next tile's queries come to L2 meanwhile
+      if (pair + kTile < t.pairs) {
+        const int rn = by_g(pair + kTile);
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(q + ((size_t)(t.first + rn) * g.Hq + (size_t)t.h * G + (pair + kTile - rn * G)) * D + side * (D / 2)));
+      }
       // ---- what the rows see
       const int pos = t.n - t.rows + r, lim = pos + 1, low = p.window > 0 ? max(lim - p.window, 0) : 0;
       const int r_first = by_g(pair0), r_last = by_g(min(pair0 + 128, t.pairs) - 1);
@@ -422,33 +442,37 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
         const int tok = t.seen.logical(page0 + j) * kPageTokens;
         const bool open = tok + kPageTokens <= lim_all && (tok >= low_all || tok + kPageTokens <= p.sinks);       // every row sees the whole page
         const int lim_t = lim - tok, low_t = low - tok, sink_t = p.sinks - tok;
-        uint32_t a[32];
+        uint32_t a[16];
         if (!open) {
           // what a row does not see becomes -infinity where it stands (pages at a mask's edge; the code below has no conditions)
 #pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
-            tmem_ld32(tS + 32 * c, a);
-            wait_ld(a);
+          for (int c = 0; c < 64; c += 32) {
 #pragma unroll
-            for (int k = 0; k < 32; ++k) {
-              const int u = 32 * c + token_at(k);
-              const bool hidden = (u >= lim_t) | ((u < low_t) & (u >= sink_t));      // (no branches)
-              a[k] = hidden ? 0xFF800000u : a[k];
+            for (int h = 0; h < 32; h += 16) {
+              tmem_ld16(tS + c + h, a);
+              wait_ld(a);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) {
+                const int u = 64 * side + c + token_at(h + k);
+                const bool hidden = (u >= lim_t) | ((u < low_t) & (u >= sink_t));    // (no branches)
+                a[k] = hidden ? 0xFF800000u : a[k];
+              }
+              tmem_st16(tS + c + h, a);
             }
-            tmem_st32(tS + 32 * c, a);
           }
           tc::tc_wait_st();
         }
         float top = -INFINITY;
 #pragma unroll 1
-        for (int c = 0; c < 128; c += 32) {
-          tmem_ld32(tS + c, a);
+        for (int c = 0; c < 64; c += 16) {
+          tmem_ld16(tS + c, a);
           wait_ld(a);
-          float t0 = max3(top, a[0], a[1]), t1 = __uint_as_float(a[2]);
+          float t0 = max3(top, a[0], a[1]), t1 = max3(__uint_as_float(a[2]), a[3], a[4]);
 #pragma unroll
-          for (int k = 3; k < 31; k += 4) { t0 = max3(t0, a[k], a[k + 1]); t1 = max3(t1, a[k + 2], a[k + 3]); }
-          top = max3(t0, __float_as_uint(t1), a[31]);
+          for (int k = 5; k < 13; k += 4) { t0 = max3(t0, a[k], a[k + 1]); t1 = max3(t1, a[k + 2], a[k + 3]); }
+          top = max3(max3(t0, a[13], a[14]), __float_as_uint(t1), a[15]);
         }
+        top = fmaxf(top, exchange(top));
         top *= fs;
         // ---- the reference moves when a logit passes it by the headroom
         const bool move = top > m + kHeadroom;       // (m = -inf: any logit at all)
@@ -458,12 +482,12 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
           if (j > 0) {
             // (nobody writes O now: this page's product has not been asked for, and S arrived behind the last one's)
 #pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-              tmem_ld32(tO + c, a);
+            for (int c = 0; c < D / 2; c += 16) {
+              tmem_ld16(tO + c, a);
               wait_ld(a);
 #pragma unroll
-              for (int k = 0; k < 32; ++k) a[k] = __float_as_uint(__uint_as_float(a[k]) * keep);
-              tmem_st32(tO + c, a);
+              for (int k = 0; k < 16; ++k) a[k] = __float_as_uint(__uint_as_float(a[k]) * keep);
+              tmem_st16(tO + c, a);
             }
           }
           l2 = mul2(l2, pack2(keep, keep));
@@ -473,20 +497,20 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
         const float base = (m == -INFINITY ? 0.f : m) - (big ? 10.0f : 0.0f);
         const f32x2 f2 = pack2(fs, fs), nb = pack2(-base, -base);
         f32x2 sum = pack2(0.f, 0.f);
-        auto weigh = [&](const uint32_t (&s)[32], uint32_t to) {
-          uint32_t w16[16];
+        auto weigh = [&](const uint32_t (&s)[16], uint32_t to) {
+          uint32_t w16[8];
 #pragma unroll
-          for (int k = 0; k < 32; k += 2) {
+          for (int k = 0; k < 16; k += 2) {
             const float2 e = unpack2(fma2(pack2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), f2, nb));
             const float2 pr = make_float2(ex2(e.x), ex2(e.y));
             sum = add2(sum, pack2(pr.x, pr.y));
             w16[k / 2] = as_u32(__floats2half2_rn(pr.x, pr.y));
           }
-          tmem_st16(to, w16);
+          tmem_st8(to, w16);
         };
 #pragma unroll 1
-        for (int c = 0; c < 128; c += 32) {
-          tmem_ld32(tS + c, a);
+        for (int c = 0; c < 64; c += 16) {
+          tmem_ld16(tS + c, a);
           wait_ld(a);
           weigh(a, tS + (c >> 1));
         }
@@ -501,7 +525,11 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       wait_warp(bO + 8 * w, seg & 1);
       ++seg;
       tc::tc_fence_after();
-      const float l = unpack2(l2).x + unpack2(l2).y;
+      float l = unpack2(l2).x + unpack2(l2).y;
+      {
+        const float other = exchange(l);
+        l = side == 0 ? l + other : other + l;       // (the same sum in both)
+      }
       const bool whole = page0 == 0 && pages == t.seen.count;
       const float inv = whole ? (l > 0.f ? 1.0f / l : 0.f) : 1.0f;
       const int slot = 2 * (int)blockIdx.x + (page0 == 0 ? 1 : 0), cr = 128 * w + row;      // (page0 > 0: the tile started in another share)
@@ -510,25 +538,27 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       {
         const long long out_row = (long long)(t.first + r) * g.Hq + (long long)t.h * G + (pair - r * G);
         const int wr = row & ~31, rows_here = min(32, t.pairs - pair0 - wr);         // (may be none)
-        uint8_t* stage = smem + sl.q + w * T::kQ + wr * 16;
-        const bool wide = !whole || out_dtype == KVQ_FP32;                           // rows of 4 D bytes: two rounds
+        constexpr int NP = D / 16;                   // pieces of a row, side and round
+        uint8_t* stage = smem + sl.q + w * T::kQ + wr * 16 + side * NP * T::kLbQ;
+        const bool wide = !whole || out_dtype == KVQ_FP32;                           // 4 bytes a channel: two rounds
+        const int step = wide ? D / 4 : D / 2;
 #pragma unroll 1
-        for (int c0 = 0; c0 < D; c0 += wide ? D / 2 : D) {
+        for (int c0 = 0; c0 < D / 2; c0 += step) {
 #pragma unroll 1
-          for (int cc = 0; cc < (wide ? D / 2 : D); cc += 32) {
-            uint32_t a[32];
-            tmem_ld32(tO + c0 + cc, a);
+          for (int cc = 0; cc < step; cc += 16) {
+            uint32_t a[16];
+            tmem_ld16(tO + c0 + cc, a);
             wait_ld(a);
             if (wide) {
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
+              for (int k = 0; k < 4; ++k) {
                 const int piece = cc / 4 + k;
                 *reinterpret_cast<float4*>(stage + piece * T::kLbQ + ((lane + piece) & 31) * 16) =
                     make_float4(__uint_as_float(a[4 * k]) * inv, __uint_as_float(a[4 * k + 1]) * inv, __uint_as_float(a[4 * k + 2]) * inv, __uint_as_float(a[4 * k + 3]) * inv);
               }
             } else {
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
+              for (int k = 0; k < 2; ++k) {
                 const int piece = cc / 8 + k;
                 uint32_t o4[4];
 #pragma unroll
@@ -540,7 +570,7 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
             }
           }
           __syncwarp();
-          constexpr int NP = D / 8;                  // pieces of a row and round
+          const int ch0 = side * (D / 2) + c0;       // first channel of the round
           // (all lanes go round as often: they ask each other where a row goes)
 #pragma unroll 4
           for (int i = 0; i < rows_here * NP; i += 32) {
@@ -549,8 +579,8 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
             const uint4 v = *reinterpret_cast<const uint4*>(stage + piece * T::kLbQ + ((rr + piece) & 31) * 16);
             uint8_t* dst;
             const long long orow = __shfl_sync(FULL, out_row, rr);
-            if (whole) dst = static_cast<uint8_t*>(out) + (orow * D + c0) * (wide ? 4 : 2);
-            else dst = reinterpret_cast<uint8_t*>(ws + ((size_t)slot * cap + 128 * w + wr + rr) * D + c0);
+            if (whole) dst = static_cast<uint8_t*>(out) + (orow * D + ch0) * (wide ? 4 : 2);
+            else dst = reinterpret_cast<uint8_t*>(ws + ((size_t)slot * cap + 128 * w + wr + rr) * D + ch0);
             *reinterpret_cast<uint4*>(dst + 16 * piece) = v;
           }
           __syncwarp();
@@ -558,28 +588,28 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       }
       tc::tc_fence_before();
       if (whole) continue;
-      if (real) *reinterpret_cast<float2*>(ws + ml_offset_floats(cap, D) + ((size_t)slot * cap + cr) * 2) = make_float2(m, l);
+      if (real && side == 0) *reinterpret_cast<float2*>(ws + ml_offset_floats(cap, D) + ((size_t)slot * cap + cr) * 2) = make_float2(m, l);
       const int first = plan.cta_of(c.xs + kGap), parts = plan.cta_of(c.xs + kGap + t.seen.count - 1) - first + 1;
       __threadfence();
-      named_bar_sync(1 + w, 128);
-      if (row == 0) const_cast<volatile int*>(sMisc)[2 + w] = (int)tagged_count(counts + 2 * first + w, id40);
-      named_bar_sync(1 + w, 128);
+      named_bar_sync(1 + w, 256);
+      if (row == 0 && side == 0) const_cast<volatile int*>(sMisc)[2 + w] = (int)tagged_count(counts + 2 * first + w, id40);
+      named_bar_sync(1 + w, 256);
       if (const_cast<volatile int*>(sMisc)[2 + w] == parts) {
         __threadfence();
         const int rows_w = min(128, t.pairs - pair0);
         const float2* mls = reinterpret_cast<const float2*>(ws + ml_offset_floats(cap, D));
         // the parts' places: the tile starts in the second one of its first CTA, goes on in the first one of those behind
         auto place = [&](int j) { return (size_t)(2 * (first + j) + (j == 0 ? 1 : 0)) * cap + 128 * w; };
-        // a thread per 16 bytes of a row, two rows of four parts in flight at a time
-        constexpr int NP = D / 4, U = 2;
+        // a thread per 16 bytes of a row, four parts in flight at a time
+        constexpr int NP = D / 4, U = 1;
 #pragma unroll 1
-        for (int idx0 = row; idx0 < rows_w * NP; idx0 += 128 * U) {
+        for (int idx0 = row + 128 * side; idx0 < rows_w * NP; idx0 += 256 * U) {
           float4 num[U];
           float ms[U], den[U];
           int rr[U];
 #pragma unroll
           for (int u = 0; u < U; ++u) {
-            rr[u] = min(idx0 + 128 * u, rows_w * NP - 1) / NP;
+            rr[u] = min(idx0 + 256 * u, rows_w * NP - 1) / NP;
             ms[u] = -INFINITY;
             den[u] = 0.f;
             num[u] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -616,7 +646,7 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
           }
 #pragma unroll
           for (int u = 0; u < U; ++u) {
-            if (idx0 + 128 * u >= rows_w * NP) break;
+            if (idx0 + 256 * u >= rows_w * NP) break;
             const float iv = den[u] > 0.f ? 1.0f / den[u] : 0.f;
             const int rw = by_g(pair0 + rr[u]);
             const size_t at = ((size_t)(t.first + rw) * g.Hq + (size_t)t.h * G + (pair0 + rr[u] - rw * G)) * D + 4 * (idx0 & (NP - 1));
@@ -630,14 +660,14 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
             }
           }
         }
-        if (row == 0) counts[2 * first + w] = 0ull;
+        if (row == 0 && side == 0) counts[2 * first + w] = 0ull;
       }
-      named_bar_sync(1 + w, 128);
+      named_bar_sync(1 + w, 256);
     }
-  } else if (warp < 24) {
+  } else if (warp < 28) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsTiles));
-    // =========================================================== pages to 16-bit tiles: two warps take a block of 32 tokens (one is bound by latency)
-    const int blk = warp & 3, half = (warp >> 2) & 1;
+    // =========================================================== pages to 16-bit tiles: by blocks of 32 tokens
+    const int blk = warp & 3;
     const int ngk = D / g.gk, ngv = D / g.gv;
     // The page to load is one ahead of the one that is written, its number was read a page earlier still.
     const uint8_t* page_ptr = nullptr;
@@ -680,12 +710,12 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       for (int e = 0; e < NI; ++e) if (e < count) m[e] = as_u32(__hmul2(as_h2(m[e]), __float2half2_rn(kBigDown)));
     };
     int it = 0;
-    if (warp < 16) {
-      // ------------------------------------------------------------ keys: half of the passes of eight tokens
+    if (warp < 24) {
+      // ------------------------------------------------------------ keys: two warps a block, half of the passes of eight tokens each
+      const int half = (warp >> 2) & 1;
       const int tl = lane & 7, ch = lane >> 3;       // token of a pass of eight (neighbours in place), quarter of its row
       constexpr int KCB = (KW < 4 ? KW : 4) * 4;
       const Codes<KB> kc;
-      const int skip_it = (int)blockIdx.x == (int)(skip_x >> 8) && skip_x >= 0 ? (int)(skip_x & 255) : -1;      // (test hook: page skip_x % 256 of CTA skip_x / 256 never arrives)
       uint32_t kw[2][KW], km[4] = {0u, 0u, 0u, 0u};
       auto load = [&]() {
 #pragma unroll
@@ -701,7 +731,7 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
           const bool wide = check_meta(km, ngk, (float)((1 << KB) - 1), there), big = bar_any(3, 256, wide);
           if (big) scale_meta(km, ngk);
           if (it >= 2) wait_warp(bKE + 8 * buf, ((it >> 1) - 1) & 1);
-          if (warp == 8 && lane == 0) sBig[it & 3] = big;
+          if (warp == 16 && lane == 0) sBig[it & 3] = big;
           uint8_t* dst = smem + sl.k + buf * T::kK;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
@@ -725,20 +755,20 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
           }
           tc::fence_async_smem();
           __syncwarp();
-          if (lane == 0 && !(it == skip_it)) mbar_arrive(bKF + 8 * buf);
+          if (lane == 0 && it != skip_x) mbar_arrive(bKF + 8 * buf);      // (skip_x: test hook - a page that never arrives)
           more = nc.on;
           if (more) { to_next(); load(); }
       }
     } else {
-      // ------------------------------------------------------------ values: one of the octets of every sixteen channels
+      // ------------------------------------------------------------ values
       const int vl = lane & 7, tq = lane >> 3;       // channel of eight, place of the chunk
       uint32_t vm[4] = {0u, 0u, 0u, 0u};
-      uint2 vw[NMW];
+      uint4 vw[NMW];
       const Codes<VB> vc;
       auto load = [&]() {
-        const uint8_t* v = page_ptr + g.v_codes_off + blk * (4 * D * VB) + (4 * vl + tq) * 16 + 8 * half;
+        const uint8_t* v = page_ptr + g.v_codes_off + blk * (4 * D * VB) + (4 * vl + tq) * 16;
 #pragma unroll
-        for (int mw = 0; mw < NMW; ++mw) vw[mw] = *reinterpret_cast<const uint2*>(v + 512 * mw);
+        for (int mw = 0; mw < NMW; ++mw) vw[mw] = *reinterpret_cast<const uint4*>(v + 512 * mw);
         load_meta(vm, g.v_meta_off, ngv);
       };
       bool more = nc.on;
@@ -748,11 +778,11 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
           const int buf = it & 1;
           const bool there = lane < tokens;
           const bool wide = check_meta(vm, ngv, (float)((1 << VB) - 1), there);
-          const bool big = bar_any(4, 256, wide);
+          const bool big = bar_any(4, 128, wide);
           if (big) scale_meta(vm, ngv);
           if (it >= 2) wait_warp(bVE + 8 * buf, ((it >> 1) - 1) & 1);
-          if (warp == 16 && lane == 0) sBig[4 + (it & 3)] = big;
-          uint8_t* dst = smem + sl.v + buf * T::kV + vl * 16 + (4 * blk + tq) * T::kLbV + 128 * half;
+          if (warp == 24 && lane == 0) sBig[4 + (it & 3)] = big;
+          uint8_t* dst = smem + sl.v + buf * T::kV + vl * 16 + (4 * blk + tq) * T::kLbV;
           __half2 s[2][2], z[2][2];                  // [half][pair of tokens]
 #pragma unroll
           for (int mw = 0; mw < NMW; ++mw) {
@@ -772,9 +802,11 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
                   }
                 }
               }
-              // the octet's words of the two token halves: bytes 0, 2 are tokens 2 tq, 2 tq + 1 of the half, bytes 1, 3 those eight further
+              // words (row half, token half): bytes 0, 2 are tokens 2 tq, 2 tq + 1 of the half, bytes 1, 3 those eight further
               *reinterpret_cast<uint4*>(dst + 2 * m16 * 128) = make_uint4(vc.values(vw[mw].x, f, s[0][0], z[0][0]), vc.values(vw[mw].x >> 8, f, s[0][1], z[0][1]),
                                                                           vc.values(vw[mw].y, f, s[1][0], z[1][0]), vc.values(vw[mw].y >> 8, f, s[1][1], z[1][1]));
+              *reinterpret_cast<uint4*>(dst + (2 * m16 + 1) * 128) = make_uint4(vc.values(vw[mw].z, f, s[0][0], z[0][0]), vc.values(vw[mw].z >> 8, f, s[0][1], z[0][1]),
+                                                                                vc.values(vw[mw].w, f, s[1][0], z[1][0]), vc.values(vw[mw].w >> 8, f, s[1][1], z[1][1]));
             }
           }
           tc::fence_async_smem();
@@ -786,7 +818,7 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
-    if (warp == 24) {
+    if (warp == 28) {
     // =========================================================== products
     // The whole warp goes along on values that it shares (counts come from one lane), so that descriptors are made on the uniform path: a
     // product per 64 cycles leaves the one thread that issues it few instructions.
@@ -807,7 +839,7 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       if (elect_one()) {
         mma_ts(d, a, b, idesc(D), add);
 #pragma unroll
-        for (int k = 1; k < 8; ++k) mma_ts(d, a + 8 * k, b + k * (2 * T::kLbV >> 4), idesc(D), 1u);
+        for (int k = 1; k < 8; ++k) mma_ts(d, a + 8 * k + (k >= 4 ? 32 : 0), b + k * (2 * T::kLbV >> 4), idesc(D), 1u);
       }
       __syncwarp();
     };
@@ -858,7 +890,7 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
   tc::tc_fence_before();
   __syncthreads();
   tc::tc_fence_after();
-  if (warp == 24) tc::tmem_dealloc(tmem, kTmemCols);
+  if (warp == 28) tc::tmem_dealloc(tmem, kTmemCols);
 }
 
 template <int D, int KB, int VB>

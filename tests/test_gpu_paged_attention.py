@@ -252,10 +252,10 @@ def test_prompt_chunks_and_decoding_in_turn(kvq):
         close(out.double().cpu().numpy(), want)
 
 
-@pytest.mark.parametrize("rows,skip", [(1, 0), (1, 3), (1, 9), (40, 2 * 256), (40, 5 * 256), (300, 2 * 256), (300, 11 * 256)])
+@pytest.mark.parametrize("rows,skip", [(1, 0), (1, 3), (1, 9), (40, 0), (300, 0), (600, 2)])
 def test_a_page_that_never_arrives_ends_the_call(kvq, rows, skip):
     """The bounded waits run out, the call ends with a status, and the next call on the same workspace is right."""
-    call = pt.Call(kvq, S(), [700, 500], [rows, 1], 0, 0, seed=15)
+    call = pt.Call(kvq, S(), [2600 if skip == 2 else 700, 500], [rows, 1], 0, 0, seed=15)
     cache, cu = call.on_gpu()
     q = call.q.cuda()
     ws = torch.empty(kvq.kvq_paged_workspace_bytes(call.cfg, rows), dtype=torch.uint8, device="cuda")
