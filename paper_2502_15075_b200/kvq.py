@@ -517,8 +517,8 @@ def kvq_paged_attention(cfg: kvq_config, cache: PagedCache, q: torch.Tensor, cu:
     assert heads == cfg.n_q_heads and dim == cfg.head_dim and out.shape == shape
     assert q.is_contiguous() and out.is_contiguous() and workspace.is_contiguous() and _DTYPE_CODES[q.dtype] == cfg.in_dtype
     _ragged(cfg, cache, cu, q, out, workspace)
-    _check(_lib.kvq_paged_attention(ctypes.byref(cfg), ctypes.byref(cache.c), q.data_ptr(), cu.data_ptr(), n, max_rows,
-                                    window, sinks, out.data_ptr(), _DTYPE_CODES[out.dtype], softmax_scale,
+    _check(_lib.kvq_paged_attention(ctypes.byref(cfg), ctypes.byref(cache.c), q.data_ptr(), cu.data_ptr(), n, int(max_rows),
+                                    int(window), int(sinks), out.data_ptr(), _DTYPE_CODES[out.dtype], float(softmax_scale),
                                     workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)),
            "kvq_paged_attention")
 

@@ -264,3 +264,47 @@ def test_a_page_that_never_arrives_ends_the_call(kvq, rows, skip):
     assert kvq.kvq_check_status(cache) == -7
     cache.status.zero_()
     close(call.got_attention(cache=cache, cu=cu, workspace=ws), call.want_attention())
+
+
+def test_pools_beyond_four_gigabytes(kvq):
+    """Pages whose offsets do not fit 32 bits, in all three operators (the rest of the pool is never touched)."""
+    sh = S()
+    for rows in (1, 50):
+        call = pt.Call(kvq, sh, [300, 200], [rows, 1], 100, 3, seed=16)
+        want, n, far = call.want_attention(), call.pages.shape[0], 200_000
+        pages = torch.empty((far + n,) + call.pages.shape[1:], dtype=torch.uint8, device="cuda")
+        assert pages.numel() > 2 ** 32
+        pages[far:] = torch.from_numpy(call.pages).cuda()
+        table = torch.where(torch.from_numpy(call.table) >= 0, torch.from_numpy(call.table) + far, -1).cuda()
+        cache = kvq.PagedCache(call.cfg, pages=pages, block_table=table, seq_len=torch.tensor(call.lens, dtype=torch.int32, device="cuda"))
+        cu = torch.from_numpy(call.cu).cuda()
+        close(call.got_attention(cache=cache, cu=cu), want)
+        near, _ = call.on_gpu()
+        outs = []
+        for c in (cache, near):
+            kvq.kvq_paged_append(call.cfg, c, call.k.cuda(), call.v.cuda(), cu)
+            kv = [torch.zeros(call.n, sh.Hkv, sh.D, dtype=sh.torch_dtype, device="cuda") for _ in range(2)]
+            kvq.kvq_paged_dequantize(call.cfg, c, cu, *kv)
+            assert kvq.kvq_check_status(c) == 0
+            outs.append(kv)
+        assert torch.equal(pages[far:], near.pages) and all(torch.equal(a, b) for a, b in zip(*outs))
+        del pages, cache
+
+
+@pytest.mark.parametrize("G", [3, 5, 7])
+@pytest.mark.parametrize("rows", [1, 100])
+def test_groups_of_heads_that_are_no_power_of_two(kvq, G, rows):
+    call = pt.Call(kvq, S(G=G, Hkv=2), [400, 130], [rows, 7], 90, 3, seed=17)
+    close(call.got_attention(), call.want_attention())
+
+
+def test_table_with_wide_rows_and_more_sequences_than_fit_a_warp(kvq):
+    """A block table whose rows lie apart, 200 sequences, and a decoding step next to a chunk in one call."""
+    lens = [40 + 3 * i for i in range(200)]
+    for rows in ([1] * 200, [1] * 199 + [60]):
+        call = pt.Call(kvq, S(D=64, gk=64, gv=64, Hkv=1, G=2, dtype="fp16"), lens, rows, 0, 0, seed=18)
+        cache, cu = call.on_gpu()
+        wide = torch.full((200, 37), -7, dtype=torch.int32, device="cuda")
+        wide[:, :call.table.shape[1]] = torch.from_numpy(call.table).cuda()
+        cache = kvq.PagedCache(call.cfg, pages=cache.pages, block_table=wide, seq_len=cache.seq_len)
+        close(call.got_attention(cache=cache, cu=cu), call.want_attention())
