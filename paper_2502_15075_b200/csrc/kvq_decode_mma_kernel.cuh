@@ -11,7 +11,7 @@ namespace mma {
 
 // Shared-memory carve-up (dynamic): ring | barriers | prefix | misc | weights | reductions | channel-wise scratch
 struct SmemLayout {
-  int page_stride, ring_bytes, bar_off, pref_off, misc_off, w_off, red_off, chan_off, total;
+  int page_stride, ring_bytes, bar_off, pref_off, src_off, misc_off, w_off, red_off, chan_off, total;
 };
 // weights: the PV operands of a page as the owners of its four 32-token blocks leave them, per value group and block
 // (16 NH bytes per lane), for two pages in turn.
@@ -20,14 +20,16 @@ struct SmemLayout {
 __host__ __device__ constexpr int weight_block_bytes(int nh) { return 512 * nh; }
 __host__ __device__ constexpr int reduction_bytes(int ngv) { return 4 * (8 * ngv * 8 + (8 + 4 + 8) * 4); }   // per warp: p z sums (64 bits), maxima, scale limit, l
 __host__ __device__ inline int chan_stage_bytes(int D, int nh) { return nh * 2 * (D / 16) * 32 * 4 + 64; }
-// prefs: words per sequence (two prefixes, pages and pages + stream gaps; a paged call also keeps its tokens, rows and first row).
+// prefs: words per sequence (two prefixes, pages and pages + stream gaps; a paged call also keeps its tokens, rows and
+// first row, and the addresses of the next 32 pages).
 __host__ __device__ inline SmemLayout smem_layout(int page_bytes, int stages, int batch, int D, int nh, int ngv, bool chan, int prefs = 2) {
   SmemLayout s;
   s.page_stride = (page_bytes + 127) & ~127;
   s.ring_bytes = s.page_stride * stages;
   s.bar_off = s.ring_bytes;
   s.pref_off = s.bar_off + 16 * 8 * 2;                      // up to 32 barriers: (full, empty[, ready]) per stage
-  s.misc_off = (s.pref_off + prefs * (batch + 1) * 4 + 15) & ~15;
+  s.src_off = (s.pref_off + prefs * (batch + 1) * 4 + 15) & ~15;
+  s.misc_off = s.src_off + (prefs > 2 ? 32 * 8 : 0);
   s.w_off = s.misc_off + 64;
   s.red_off = s.w_off + 2 * ngv * 4 * weight_block_bytes(nh);
   s.chan_off = s.red_off + reduction_bytes(ngv);
@@ -644,53 +646,57 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
     return SeenPages{0, 0, 0};
   };
   // =========================================================== producer warp
-  // Paged: the lanes hold the pool pages of the next 32 pages of the share, and those of the 32 behind are on their way, so that a page
-  // costs no look-up; a new sequence starts anew (16 streams x 32,767 tokens of the 8B shape, looked up when they are needed: 86 us; PAGED_US).
+  // Paged: by batches of up to 32 pages of a sequence.  The lanes make a batch's addresses together while the pool pages of the next one are on
+  // their way, then one lane issues the copies, with few instructions a page beside the consumer warp on its quarter of the SM (16 streams x
+  // 32,767 tokens of the 8B shape / 4 x 131,071 of the 70B: a look-up when a page is needed 86 us / 121, 32 ahead by shuffles 75.4 / 124.2, so 74.9 / 118.6; pages in
+  // one piece per stream, kvq_decode_attention, 72.1 / 115.2).
   if constexpr (PAGED) {
     if (warp == NW) {
-      int it = 0, stage = 0, ids = 0, ids_behind = 0, ids_x = 0, ids_b = -1;
+      unsigned long long* src = reinterpret_cast<unsigned long long*>(smem + sl.src_off);
+      int it = 0, stage = 0, ids = 0, ids_b = -1, x = x_lo;
       uint32_t phase = 1;                // parity of the previous round of `empty`
       bool ok = true;
       const uint64_t policy = l2_evict_first_policy();
       SeenPages seen{0, 0, 0};
-      for (int x = x_lo; x < x_hi; ++x, ++it) {
-        // the k-th page from here on, of this sequence (head after head it has the same pages)
+      while (x < x_hi && ok) {
+        const int left = min(x_hi - x, (Hkv - h) * pages_b - page), n = min(left, 32);       // (head after head a sequence has the same pages)
         auto look_up = [&](int k) { return pool_page(pa, b, seen.logical((page + k) % pages_b)); };
         if (b != ids_b) {
-          ids_b = b; ids_x = x;
+          ids_b = b;
           seen = seen_of(b);
           ids = look_up(lane);
-          ids_behind = look_up(32 + lane);
-        } else if (x - ids_x == 32) {
-          ids_x = x;
-          ids = ids_behind;
-          ids_behind = look_up(32 + lane);
         }
-        int id = __shfl_sync(FULL, ids, x - ids_x);
-        if (id < 0) {                    // outside the pool: another page is read in its place
-          if (lane == 0) atomicOr(c.status, KVQ_STATUS_BAD_INPUT);
-          id = 0;
-        }
-        if (it >= stages) {
-          bool free_ = true;
-          if (lane == 0) free_ = mbar_wait(bar0 + 8 * (stages + stage), phase, wait_ns) && !*abort_flag;
-          ok = __all_sync(FULL, free_);
-          if (!ok) break;
-        }
-        if (lane == 0 && x != skip_x) {          // (skip_x: test hook - a page that never arrives makes the consumers' bounded wait expire)
-          const uint32_t fb = bar0 + 8 * stage;
-          mbar_expect_tx(fb, (uint32_t)g.page_bytes);
-          bulk_load(ring + stage * sl.page_stride, pa.pages + ((size_t)id * Hkv + h) * (size_t)g.page_bytes, (uint32_t)g.page_bytes, fb, policy);
-        }
-        __syncwarp();
-        if (++stage == stages) { stage = 0; phase ^= 1; }
-        if (++page == pages_b) {
-          page = 0;
-          if (++h == Hkv) {
-            h = 0;
-            do { ++b; } while (b < B && sPref[b + 1] == sPref[b]);
-            if (b < B) pages_b = (sPref[b + 1] - sPref[b]) / Hkv;
+        if (lane < n) {
+          int id = ids;
+          if (id < 0) {                  // outside the pool: another page is read in its place
+            atomicOr(c.status, KVQ_STATUS_BAD_INPUT);
+            id = 0;
           }
+          src[lane] = reinterpret_cast<unsigned long long>(pa.pages) + ((size_t)id * Hkv + h + (page + lane) / pages_b) * (size_t)g.page_bytes;
+        }
+        if (left > 32) ids = look_up(32 + lane);
+        __syncwarp();
+        if (lane == 0) {
+#pragma unroll 1
+          for (int k = 0; k < n; ++k, ++it) {
+            if (it >= stages && !(mbar_wait(bar0 + 8 * (stages + stage), phase, wait_ns) && !*abort_flag)) { ok = false; break; }
+            if (x + k != skip_x) {       // (skip_x: test hook - a page that never arrives makes the consumers' bounded wait expire)
+              const uint32_t fb = bar0 + 8 * stage;
+              mbar_expect_tx(fb, (uint32_t)g.page_bytes);
+              bulk_load(ring + stage * sl.page_stride, reinterpret_cast<const void*>(src[k]), (uint32_t)g.page_bytes, fb, policy);
+            }
+            if (++stage == stages) { stage = 0; phase ^= 1; }
+          }
+        }
+        ok = __shfl_sync(FULL, ok, 0);   // (and the addresses may be written again)
+        x += n;
+        page += n;
+        h += page / pages_b;
+        page %= pages_b;
+        if (h == Hkv) {
+          h = 0;
+          do { ++b; } while (b < B && sPref[b + 1] == sPref[b]);
+          if (b < B) pages_b = (sPref[b + 1] - sPref[b]) / Hkv;
         }
       }
       if (lane == 0) {
@@ -975,6 +981,14 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
     // a block is unmasked when all of its 32 tokens exist and every query row may see them (several causal rows:
     // row r sees the first n - (rows - 1 - r) tokens of the n the sequence holds, window included)
     const int n_unmasked = min(n_tok, n_all - (rows - 1));
+    // the segment's pages that need no masks: those inside the window, and those inside the first tokens (all in front of the window)
+    [[maybe_unused]] int full_from = 0, full_to = 0, full_sink = 0;
+    if constexpr (PAGED) {
+      full_from = max(seen.first, ((low_all + kPageTokens - 1) >> 7) - seen.skip) - page;
+      full_to = (n_unmasked >> 7) - seen.skip - page;
+      full_sink = min(seen.first, pa_sinks >> 7) - page;
+    }
+
     const int stream = b * Hkv + h;
     // the queries are on their way while one warp works out
     [[maybe_unused]] uint2 q_raw[NH][NR];
@@ -1404,9 +1418,8 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
         if (!__all_sync(FULL, mbar_try_wait(bar0 + 8 * (2 * stages + stage), phase))) wait_slowly(bar0 + 8 * (2 * stages + stage));
       }
       // a page whose tokens all exist and may be seen by every query row needs no masks
-      const int tok_page = PAGED ? seen.logical(page + pp) * kPageTokens : (page + pp) * kPageTokens;
-      const bool below = PAGED && tok_page < low_all && tok_page + kPageTokens > pa_sinks;       // the window ends inside the page
-      if (tok_page + kPageTokens <= n_unmasked && !below) process(std::true_type{}, pp);
+      const bool full = PAGED ? (pp >= full_from && pp < full_to) || pp < full_sink : (page + pp + 1) * kPageTokens <= n_unmasked;
+      if (full) process(std::true_type{}, pp);
       else process(std::false_type{}, pp);
       __syncwarp();
       mbar_arrive_if(bar0 + 8 * (stages + stage), lane == 0);
