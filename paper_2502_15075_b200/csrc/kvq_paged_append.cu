@@ -2,7 +2,8 @@
 // group) and packing into the pages that a block table names.
 //
 // A row (one head of one token) is spread over D / 8 lanes, eight consecutive channels each: half-split pairs are a shuffle apart, interleaved
-// ones sit in a lane, and a group's minimum and maximum are a few shuffles.
+// ones sit in a lane, and a group's minimum and maximum are a few shuffles.  8B shape with queries, K4V2: a token each for 64 sequences 3.9 us (a
+// replayed graph), prompts of 4 x 8,192 tokens 163 us for 0.70 GB (keys and queries 150 with two thirds of the issue slots, values 22).
 #include "kvq_paged.cuh"
 #include "kvq_quantize.cuh"
 
@@ -86,7 +87,7 @@ __device__ __forceinline__ void rotate_row(float (&x)[8], const RopeArgs& r, con
 
 // Rows of a token: n_kv_heads keys, as many values where V_ROWS, then the query heads.  A warp takes 256 / D of them at a time and
 // `groups` such in a row, the next two's loads in flight: the token's angles stay in registers.
-// Long calls are bound by the memory system (8B shape, 32,768 tokens: see launch_paged_append), single tokens by latency.
+// Long calls are bound by issue and by memory, single tokens by latency.
 // KB: the keys' width in calls whose values go by blocks (no value rows here), 0: read from the geometry.
 template <int D, int DTYPE, int KB>
 __global__ void __launch_bounds__(kThreads, 4)
@@ -229,8 +230,11 @@ int launch_paged_append(const Geom& g, const Paged& p, const void* k, const void
                         const RopeArgs& rope, const void* q, int64_t q_row, int64_t q_head, void* q_out, cudaStream_t stream) {
   const AppendArgs a{static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), static_cast<const uint16_t*>(q),
                      static_cast<uint16_t*>(q_out), kv_row, kv_head, q_row, q_head, rope};
-  // Values go by token rows (their codes then leave byte by byte) in short calls, by blocks of tokens in a launch of their own in long ones.
-  const bool blocks = p.n_rows >= 8 * g.B && p.n_rows >= 64;
+  // Values go by token rows (their codes then leave byte by byte) in short calls, by blocks of tokens in a launch of their own in long ones, where
+  // most blocks are full. Measured with 8 heads of each kind, rows | blocks: D 128, 1 x 2 tokens 3.0 | 5.4 us, 8 x 64 tokens 9.5 | 10.7,
+  // 64 x 16 tokens 13.2 | 14.1, 8 x 256 tokens 23.3 | 20.0, 64 x 32 tokens 23.5 | 20.8, 64 x 256 tokens 107 | 91; D 64, 8 x 256 tokens 12.4 | 13.5,
+  // 64 x 64 tokens 19.7 | 19.1. They meet between one and two million values.
+  const bool blocks = (long long)p.n_rows * g.Hkv * g.D >= 3ll << 19 && p.n_rows >= 16ll * g.B;
   const int rpw = 256 / g.D, per_token = (blocks ? 1 : 2) * ((g.Hkv + rpw - 1) / rpw) + (q ? (g.Hq + rpw - 1) / rpw : 0);
   // enough warps to fill the GPU twice, then longer ones
   const long long warps = (long long)p.n_rows * per_token;

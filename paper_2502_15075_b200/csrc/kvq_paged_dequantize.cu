@@ -4,7 +4,8 @@
 // A warp takes one block of 32 tokens of one head and one side.  Keys go from global to global memory: a lane owns a quarter of a
 // token's row, whose bytes are four consecutive channels of every 16-channel slice, and four lanes write 32 contiguous bytes.  Values
 // are transposed by stmatrix into a padded tile of the warp's own and leave as whole rows.  Code bytes become floats by a byte
-// permute and an exact subtraction.  Bound by the 16-bit stores, which are 4 to 8 times what is read.
+// permute and an exact subtraction.  Bound by the 16-bit stores, which are 4 to 8 times what is read: 4 x up to 8,001 tokens of the 8B shape K4V2 27 us
+// (element by element 254), 32,768 tokens 36.6 us (161 MB, 0.67 of the copy rate).
 #include "kvq_paged.cuh"
 
 namespace kvq {

@@ -75,6 +75,43 @@ def test_append_rotated_is_exact(kvq, sh, lens, rows):
     run_append(call, sh.D, False)
 
 
+def long_call(sh):
+    """Rows behind the last sequence that make a call as long as those whose values are stored by blocks of tokens."""
+    return (3 << 19) // (sh.Hkv * sh.D) + 1
+
+
+@pytest.mark.parametrize("lens,rows", CALLS)
+@pytest.mark.parametrize("sh", SHAPES, ids=str)
+def test_long_append_is_exact(kvq, sh, lens, rows):
+    call = pt.Call(kvq, sh, lens, rows, pad=long_call(sh), seed=len(lens), fill=False, keys=3.0)
+    run_append(call, sh.D, False)
+
+
+@pytest.mark.parametrize("sh", [S(), S(D=64, gk=64, gv=32, vb=4, dtype="fp16")], ids=str)
+def test_long_append_full_of_rows(kvq, sh):
+    n = long_call(sh)
+    lens = [n // 2 + 70, 300, 0, n // 2 + 1]
+    run_append(pt.Call(kvq, sh, lens, [n // 2, 300, 0, n // 2 + 1], pad=0, seed=17, fill=False), 32, True)
+
+
+@pytest.mark.parametrize("only", ["k", "v"])
+def test_one_side_read_back(kvq, only):
+    """Keys alone or values alone, into the middle of a buffer, twice: what both together give, and nothing beside it."""
+    sh = S(Hkv=3, G=1)
+    call = pt.Call(kvq, sh, [300, 131], [290, 131], seed=18, pad=4)
+    cache, cu = call.on_gpu()
+    both = [torch.zeros(call.n, sh.Hkv, sh.D, dtype=sh.torch_dtype, device="cuda") for _ in range(2)]
+    kvq.kvq_paged_dequantize(call.cfg, cache, cu, *both)
+    wide = torch.full((call.n + 2, sh.Hkv, sh.D), 7.0, dtype=sh.torch_dtype, device="cuda")
+    part = wide[1:1 + call.n]
+    for _ in range(2):
+        kvq.kvq_paged_dequantize(call.cfg, cache, cu, part if only == "k" else None, part if only == "v" else None)
+    assert kvq.kvq_check_status(cache) == 0
+    real = int(call.cu[-1])
+    assert torch.equal(part[:real], both[only == "v"][:real])
+    assert bool((wide[0] == 7).all()) and bool((wide[1 + real:] == 7).all())
+
+
 @pytest.mark.parametrize("rotary", [0, 16, 48, 64, 96, 128])
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_partial_and_interleaved_rotation(kvq, rotary, interleaved):
@@ -125,9 +162,10 @@ def test_appends_token_by_token_equal_one_append(kvq):
         assert torch.equal(cache.pages, want)
 
 
-def test_device_side_refusals_set_the_status_and_write_nothing(kvq):
+@pytest.mark.parametrize("pad", [0, long_call(S())])
+def test_device_side_refusals_set_the_status_and_write_nothing(kvq, pad):
     sh = S()
-    call = pt.Call(kvq, sh, [200, 130], [3, 2], seed=12, fill=False, capacity=256)
+    call = pt.Call(kvq, sh, [200, 130], [3, 2], pad=pad, seed=12, fill=False, capacity=256)
     BAD = kvq.STATUS_BAD_INPUT
     cos, sin = pt.tables(128, 256)
     rope = kvq.Rope(torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda())
@@ -150,7 +188,7 @@ def test_device_side_refusals_set_the_status_and_write_nothing(kvq):
     attempt(lambda c, cu: c.seq_len.copy_(torch.tensor([-5, -2**31], dtype=torch.int32)))
     attempt(lambda c, cu: c.block_table.fill_(10 ** 6))                                       # outside the pool
     attempt(lambda c, cu: c.block_table.fill_(-1))
-    attempt(lambda c, cu: cu.copy_(torch.tensor([0, 9, 3], dtype=torch.int32)))               # not monotonic, beyond the rows
+    attempt(lambda c, cu: cu.copy_(torch.tensor([0, call.n + 4, 3], dtype=torch.int32)))               # not monotonic, beyond the rows
     attempt(lambda c, cu: cu.copy_(torch.tensor([-4, 2**31 - 1, 2**31 - 1], dtype=torch.int32)))
     short = kvq.Rope(rope.cos[:130].contiguous(), rope.sin[:130].contiguous())
     attempt(lambda c, cu: None, short, untouched=False)     # the second sequence fits the rotation's table, the first does not

@@ -1,4 +1,8 @@
 """kvq_paged_attention against fp64 NumPy on the same packed bytes: window, first tokens, ragged rows, layouts, refusals."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -308,3 +312,72 @@ def test_table_with_wide_rows_and_more_sequences_than_fit_a_warp(kvq):
         wide[:, :call.table.shape[1]] = torch.from_numpy(call.table).cuda()
         cache = kvq.PagedCache(call.cfg, pages=cache.pages, block_table=wide, seq_len=cache.seq_len)
         close(call.got_attention(cache=cache, cu=cu), call.want_attention())
+
+
+@pytest.mark.parametrize("pairs", [((1, 60), (2, 1)), ((300, 4), (1, 1)), ((40, 40), (3, 300))])
+def test_two_streams_with_workspaces_of_their_own(kvq, pairs):
+    """Calls of both kernels at once on one pool, each stream with its own workspace: as alone."""
+    call = [[pt.Call(kvq, S(), [1900, 700], [r, 1], 0, 0, seed=30 + r) for r in rows] for rows in pairs]
+    streams = [torch.cuda.Stream() for _ in pairs]
+    jobs = []
+    for i in range(2):
+        for c in call[i]:
+            cache, cu = c.on_gpu()
+            ws = torch.empty(kvq.kvq_paged_workspace_bytes(c.cfg, max(c.rows)), dtype=torch.uint8, device="cuda")
+            jobs.append((streams[i], c, cache, cu, c.q.cuda(), ws, [torch.zeros(c.q.shape, device="cuda") for _ in range(4)]))
+    torch.cuda.synchronize()
+    for k in range(4):
+        for s, c, cache, cu, q, ws, outs in jobs:
+            kvq.kvq_paged_attention(c.cfg, cache, q, cu, outs[k], ws, max(c.rows), stream=s)
+    torch.cuda.synchronize()
+    for s, c, cache, cu, q, ws, outs in jobs:
+        assert kvq.kvq_check_status(cache) == 0
+        want = c.got_attention(out_fill=0.0)
+        for out in outs:
+            assert np.array_equal(out.double().cpu().numpy(), want)
+
+
+def test_one_workspace_for_calls_of_every_kind(kvq):
+    """Decoding, chunks of several lengths and other windows in turn on one stream and one workspace, as a server that mixes them."""
+    shared = None
+    calls = [pt.Call(kvq, S(), [1500, 900], r, w, s, seed=40 + i)
+             for i, (r, w, s) in enumerate((([1, 1], 0, 0), ([300, 7], 0, 0), ([2, 1], 200, 4), ([600, 600], 333, 1), ([1, 0], 0, 0)))]
+    need = max(kvq.kvq_paged_workspace_bytes(c.cfg, max(c.rows)) for c in calls)
+    shared = torch.full((need,), 171, dtype=torch.uint8, device="cuda")
+    alone = [c.got_attention() for c in calls]
+    for i in (0, 1, 2, 3, 4, 1, 0, 3, 2, 2, 1, 1, 4):
+        assert np.array_equal(calls[i].got_attention(workspace=shared), alone[i])
+
+
+def test_first_calls_of_a_process_may_be_captured(tmp_path):
+    """No warm-up outside the capture: append, both attention kernels and the read-back recorded first of all, then replayed."""
+    here = os.path.dirname(os.path.abspath(__file__))
+    code = """
+import sys; sys.path[:0] = [%r, %r]
+import numpy as np, torch, paged_testlib as pt
+from paper_2502_15075_b200 import kvq
+calls = [pt.Call(kvq, pt.Shape(), [700, 200], [r, 1], seed=r) for r in (1, 40)]
+jobs = []
+for c in calls:
+    cache, cu = c.on_gpu()
+    ws = torch.empty(kvq.kvq_paged_workspace_bytes(c.cfg, max(c.rows)), dtype=torch.uint8, device="cuda")
+    q = c.q.cuda(); kv = [x.cuda() for x in (c.k, c.v)]
+    jobs.append((c, cache, cu, ws, q, torch.full(q.shape, 0.5, device="cuda"), kv, [torch.zeros_like(x) for x in kv]))
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    for c, cache, cu, ws, q, out, kv, back in jobs:
+        kvq.kvq_paged_attention(c.cfg, cache, q, cu, out, ws, max(c.rows))
+        kvq.kvq_paged_append(c.cfg, cache, kv[0], kv[1], cu)
+        kvq.kvq_paged_dequantize(c.cfg, cache, cu, back[0], back[1])
+g.replay()
+torch.cuda.synchronize()
+for c, cache, cu, ws, q, out, kv, back in jobs:
+    assert kvq.kvq_check_status(cache) == 0
+    assert np.array_equal(out.double().cpu().numpy(), c.got_attention())
+    again = [torch.zeros_like(x) for x in back]
+    kvq.kvq_paged_dequantize(c.cfg, cache, cu, again[0], again[1])
+    assert torch.equal(back[0], again[0]) and torch.equal(back[1], again[1]) and bool(back[0].any())
+""" % (os.path.dirname(here), here)
+    res = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, res.stderr[-3000:]
