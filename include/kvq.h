@@ -315,8 +315,9 @@ int kvq_paged_append(const kvq_config* cfg, const kvq_paged_cache* cache, const 
  *     KVQ_FP16/BF16/FP32).
  *   max_rows: no sequence has more rows in this call (1: a decoding step); sizes the workspace and chooses the kernel.  Up to
  *     n_q_heads / n_kv_heads * max_rows = 8 (row, head) pairs per KV head are served by the kernel behind kvq_decode_attention where it
- *     is built for the configuration, everything else by one that makes 16-bit tiles of the pages for the tensor cores; a batch
- *     of long chunks and single tokens is faster as two calls.
+ *     is built for the configuration, some more rows over long caches by several launches of it (capacity and window tell, so a
+ *     capacity far above the lengths costs such calls time), everything else by one that makes 16-bit tiles of the pages for the
+ *     tensor cores; a batch of long chunks and single tokens is faster as two calls.
  *   softmax_scale <= 0 selects 1/sqrt(head_dim).
  *   workspace: device scratch of at least kvq_paged_workspace_bytes(), 16-byte aligned, contents arbitrary.  Calls that may
  *     overlap on the GPU need separate ones.

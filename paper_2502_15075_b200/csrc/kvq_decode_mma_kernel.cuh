@@ -543,7 +543,7 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
       if constexpr (PAGED) {
         if (i < B) {
           bool bad;
-          const SeqRows s = seq_rows(pa, i, g.capacity, g.rows, bad);
+          const SeqRows s = part_of(seq_rows(pa, i, g.capacity, pa.max_rows, bad), pa.from, g.rows);
           if (bad) atomicOr(c.status, KVQ_STATUS_BAD_INPUT);
           if (s.rows > 0) pages = seen_pages(s.n - s.rows, s.n - 1, pa.window, pa.sinks).count;
           sSeq[3 * i] = s.n; sSeq[3 * i + 1] = s.rows; sSeq[3 * i + 2] = s.first;
@@ -636,6 +636,13 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
   volatile int* abort_flag = sMisc + 1;
   volatile int* n_published = sMisc + 2;      // count returned for the partial just published
   const unsigned long long id40 = (call_id & 0xFFFFFFFFFFull) ? (call_id & 0xFFFFFFFFFFull) : 1ull;
+
+  // The streams' count words: behind the partials; paged, in front of them, where they lie alike for calls of any number of rows (words that
+  // another call's partials have overwritten are swapped for one CTA after the other: one sequence of 32,767 tokens 16 -> 41 us).
+  auto count_words = [&]() {
+    if constexpr (PAGED) return reinterpret_cast<unsigned long long*>(ws) - B * Hkv;
+    return reinterpret_cast<unsigned long long*>(ws + tag_offset_floats(B * Hkv, s_cap, G, D));
+  };
 
   // What a sequence's rows see of its pages.
   [[maybe_unused]] auto seen_of = [&](int bb) {
@@ -1086,7 +1093,7 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
     // tokens 328 -> 313, eight ragged K4V4 layers 166 -> 150, 70B-shaped 247 -> 239.  (By another thread than the bookkeeping's and
     // behind the queries: 1 to 2 % of a short step.  A word with other contents is started when it is counted in, see tagged_count.)
     if (tid_ == 32 && (seg_pages < pages_b || n_all > n_tok))
-      atomicCAS(reinterpret_cast<unsigned long long*>(ws + tag_offset_floats(B * Hkv, s_cap, G, D)) + stream, 0ull, id40 << 24);
+      atomicCAS(count_words() + stream, 0ull, id40 << 24);
 
     auto process = [&](auto full_tag, int pp) {
       constexpr bool FULL_PAGE = decltype(full_tag)::value;
@@ -1489,7 +1496,7 @@ decode_mma_kernel(Geom g, CachePtrs c, const uint16_t* __restrict__ q, float c1,
         if (!direct) {
           __threadfence();
           named_bar_sync(1, NCONS);
-          unsigned long long* counts = reinterpret_cast<unsigned long long*>(ws + tag_offset_floats(B * Hkv, s_cap, G, D));
+          unsigned long long* counts = count_words();
           if (tid_ == 0) *n_published = (int)tagged_count(counts + stream, id40);
           named_bar_sync(1, NCONS);
           if (*n_published == (WIN ? sMisc[3] : n_part)) {

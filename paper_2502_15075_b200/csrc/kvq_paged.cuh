@@ -16,6 +16,7 @@ struct Paged {
   uint32_t* status;
   int n_pool, n_rows;
   int max_rows, window, sinks;      // attention only (window 0: none)
+  int from;                         // decode kernel: the launch serves each sequence's rows from .. from + g.rows - 1
 };
 
 struct RopeArgs { const float *cos, *sin; int n_positions, half, interleaved; };      // half: rotary_dim / 2, 0 without a rotation
@@ -29,6 +30,12 @@ __device__ __forceinline__ SeqRows seq_rows(const Paged& p, int b, int limit, in
   bad = c0 < 0 || c1 < c0 || c1 > p.n_rows || n < 0 || n > limit;
   bad = bad || c1 - c0 > n || c1 - c0 > max_rows;
   return SeqRows{bad ? 0 : n, bad ? 0 : c1 - c0, bad ? 0 : c0};
+}
+
+// Its rows from .. from + most - 1 alone: as a call of just these tokens.
+__device__ __forceinline__ SeqRows part_of(const SeqRows& s, int from, int most) {
+  const int rows = min(max(s.rows - from, 0), most);
+  return SeqRows{rows > 0 ? s.n - (s.rows - from - rows) : s.n, rows, s.first + from};
 }
 
 // The sequence of row i: the number of ends cu[1 ..] at or below it.  The whole warp asks for the same row.
@@ -98,8 +105,9 @@ __host__ __device__ __forceinline__ SeenPages seen_pages(int p0, int p1, int win
 int launch_paged_append(const Geom& g, const Paged& p, const void* k, const void* v, int64_t kv_row, int64_t kv_head,
                         const RopeArgs& rope, const void* q, int64_t q_row, int64_t q_head, void* q_out, cudaStream_t stream);
 int launch_paged_dequantize(const Geom& g, const Paged& p, void* k_out, void* v_out, cudaStream_t stream);
-// up to eight (row, head) pairs per KV head (g.rows: the most rows of a sequence)
-bool paged_decode_supported(const Geom& g);
+// few rows (g.rows: the most rows of a sequence), where it serves the call; bytes of workspace behind the count words for any window
+bool paged_decode_serves(const Geom& g, const Paged& p);
+size_t paged_decode_workspace_bytes(const Geom& g);
 int launch_paged_decode(const Geom& g, const Paged& p, const void* q, void* out, int out_dtype, float scale_log2e, float* ws,
                         const DecodeDebug& dbg, cudaStream_t stream);
 // any number of rows

@@ -26,7 +26,7 @@ int paged_args(const Geom& g, const kvq_paged_cache* c, const int32_t* cu, int32
   if (c->n_pages < 1 || c->table_stride < g.n_pages || n_rows < 0) return KVQ_ERR_INVALID_ARG;
   if (!aligned16(c->pages)) return KVQ_ERR_MISALIGNED;
   *p = Paged{static_cast<uint8_t*>(c->pages), c->block_table, c->table_stride, c->seq_len, cu, reinterpret_cast<uint32_t*>(c->status),
-             c->n_pages, n_rows, 0, 0, 0};
+             c->n_pages, n_rows, 0, 0, 0, 0};
   return KVQ_OK;
 }
 
@@ -34,6 +34,13 @@ int paged_args(const Geom& g, const kvq_paged_cache* c, const int32_t* cu, int32
 int rows_ok(const Geom& g, const void* x, int64_t row, int64_t head, int heads, int n_rows) {
   if ((n_rows > 1 && row < g.D) || (heads > 1 && head < g.D)) return KVQ_ERR_INVALID_ARG;
   return !aligned16(x) || (n_rows > 1 && row % 8) || (heads > 1 && head % 8) ? KVQ_ERR_MISALIGNED : KVQ_OK;
+}
+
+// The workspace begins with the decode kernel's count words, one per stream, whichever kernel serves the call; the last ones end at a multiple of 16.
+size_t count_words_bytes(const Geom& g) { return ((size_t)g.B * g.Hkv * 8 + 15) & ~(size_t)15; }
+size_t paged_workspace_bytes(const Geom& g) {
+  const size_t decode = paged_decode_workspace_bytes(g), chunk = paged_chunk_workspace_bytes(g);
+  return count_words_bytes(g) + (decode > chunk ? decode : chunk);
 }
 
 int attention_with(const DecodeDebug& dbg, const kvq_config* cfg, const kvq_paged_cache* cache, const void* q, const int32_t* cu, int32_t n_rows,
@@ -49,19 +56,16 @@ int attention_with(const DecodeDebug& dbg, const kvq_config* cfg, const kvq_page
   if (!q || !out || !workspace) return KVQ_ERR_INVALID_ARG;
   if (out_dtype != KVQ_FP16 && out_dtype != KVQ_BF16 && out_dtype != KVQ_FP32) return KVQ_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return KVQ_ERR_MISALIGNED;
-  size_t need = 0;
-  rc = kvq_paged_workspace_bytes(cfg, max_rows, &need);
-  if (rc != KVQ_OK) return rc;
-  if (workspace_bytes < need) return KVQ_ERR_WORKSPACE_TOO_SMALL;
   g.rows = max_rows;
   p.max_rows = max_rows;
   p.window = window;
   p.sinks = sinks;
+  if (workspace_bytes < paged_workspace_bytes(g)) return KVQ_ERR_WORKSPACE_TOO_SMALL;
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)g.D);
   const float c1 = scale * 1.4426950408889634f;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  auto launch = paged_decode_supported(g) ? launch_paged_decode : launch_paged_chunk;
-  return launch(g, p, q, out, out_dtype, c1, static_cast<float*>(workspace), dbg, stream);
+  auto launch = paged_decode_serves(g, p) ? launch_paged_decode : launch_paged_chunk;
+  return launch(g, p, q, out, out_dtype, c1, reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + count_words_bytes(g)), dbg, stream);
 }
 
 }  // namespace
@@ -103,7 +107,7 @@ int kvq_paged_workspace_bytes(const kvq_config* cfg, int32_t max_rows, size_t* o
   if (rc != KVQ_OK) return rc;
   if (!out || max_rows < 1) return KVQ_ERR_INVALID_ARG;
   g.rows = max_rows;
-  *out = paged_decode_supported(g) ? flat_workspace_bytes(g) : paged_chunk_workspace_bytes(g);
+  *out = paged_workspace_bytes(g);
   return KVQ_OK;
 }
 

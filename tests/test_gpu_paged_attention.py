@@ -381,3 +381,29 @@ for c, cache, cu, ws, q, out, kv, back in jobs:
 """ % (os.path.dirname(here), here)
     res = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
     assert res.returncode == 0, res.stderr[-3000:]
+
+
+@pytest.mark.parametrize("sh,rows,capacity", [
+    (S(Hkv=8), [4, 1, 0, 3], 8192), (S(Hkv=8), [3, 3, 2, 1], 8192), (S(Hkv=8), [6, 5, 1, 2], 16384), (S(Hkv=8), [8, 3, 7, 0], 32768),
+    (S(Hkv=8), [9, 10, 1, 0], 196608), (S(Hkv=8, G=8), [2, 1, 2, 0], 8192), (S(Hkv=4, G=3), [4, 3, 1, 1], 16384), (S(Hkv=8, G=1), [13, 9, 8, 1], 8192),
+    (S(Hkv=8, gk=32, gv=128), [2, 1, 0, 2], 8192), (S(D=64, gk=64, gv=64, dtype="fp16", Hkv=8, G=2), [7, 5, 4, 1], 8192)], ids=str)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (7000, 5), (130, 4)])
+def test_few_rows_over_large_capacities(kvq, sh, rows, capacity, window, sinks):
+    """More pairs than one launch of the decode kernel takes, on capacities and windows where several serve the call and where they do
+    not; a sequence's rows lie in all launches, in the first ones, in none."""
+    call = pt.Call(kvq, sh, [500, 257, 130, 16], rows, window, sinks, pad=2, seed=50 + max(rows), capacity=capacity, keys=2.0)
+    got = call.got_attention()
+    close(got, call.want_attention())
+    assert np.array_equal(got, call.got_attention())
+
+
+def test_more_rows_than_announced_are_passed_over_by_every_launch(kvq):
+    call = pt.Call(kvq, S(Hkv=8), [400, 300, 200], [5, 4, 1], 0, 0, seed=61, capacity=16384)
+    cache, cu = call.on_gpu()
+    ws = torch.empty(kvq.kvq_paged_workspace_bytes(call.cfg, 4), dtype=torch.uint8, device="cuda")
+    out = torch.full(call.q.shape, 0.5, dtype=torch.float32, device="cuda")
+    kvq.kvq_paged_attention(call.cfg, cache, call.q.cuda(), cu, out, ws, 4)
+    assert int(cache.status) == kvq.STATUS_BAD_INPUT
+    got = out.double().cpu().numpy()
+    assert np.all(got[:5] == 0.5)
+    close(got[5:], call.want_attention()[5:])
