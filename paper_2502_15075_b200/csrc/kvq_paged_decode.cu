@@ -49,7 +49,7 @@ int rows_per_launch(const Geom& g, const Paged& p) {
     part.rows = g.rows < pairs / g.G ? g.rows : pairs / g.G;
     if (part.rows < 1) continue;
     const long long launches = (g.rows + part.rows - 1) / part.rows;
-    if (launches > 1 && launches * (9 * 1480 + 5 * pages) >= 13 * 1480 + 26 * pages) continue;
+    if (launches > 5 || (launches > 1 && launches * (9 * 1480 + 5 * pages) >= 13 * 1480 + 26 * pages)) continue;      // (26 / 5: six never win)
     if (pick_paged(part, p, nullptr, 0.f, nullptr, nullptr, 0, DecodeDebug{}, nullptr, true) == KVQ_OK) return part.rows;
   }
   return 0;

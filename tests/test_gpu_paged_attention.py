@@ -407,3 +407,12 @@ def test_more_rows_than_announced_are_passed_over_by_every_launch(kvq):
     got = out.double().cpu().numpy()
     assert np.all(got[:5] == 0.5)
     close(got[5:], call.want_attention()[5:])
+
+
+@pytest.mark.parametrize("rows", [1, 3])
+@pytest.mark.parametrize("sh", [S(Hkv=1), S(Hkv=1, D=64, gk=64, gv=64)], ids=str)
+def test_largest_batch(kvq, sh, rows):
+    rng = np.random.default_rng(70)
+    lens = [int(x) for x in rng.integers(0, 20, 1024)]
+    call = pt.Call(kvq, sh, lens, [min(n, rows) for n in lens], 9, 1, pad=3, seed=71)
+    close(call.got_attention(), call.want_attention())
