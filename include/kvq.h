@@ -313,7 +313,7 @@ int kvq_paged_append(const kvq_config* cfg, const kvq_paged_cache* cache, const 
  * first `sinks` tokens stay visible.  Pages that no row of the call sees are not read: their table entries may be anything.
  *   q, out: device, [n_rows][n_q_heads][head_dim] contiguous, 16-byte aligned, not overlapping (q in_dtype, out out_dtype:
  *     KVQ_FP16/BF16/FP32).
- *   max_rows: no sequence has more rows in this call (1: a decoding step); sizes the workspace and chooses the kernel.  Up to
+ *   max_rows: no sequence has more rows in this call (1: a decoding step; values beyond capacity_tokens count as it); sizes the workspace and chooses the kernel.  Up to
  *     n_q_heads / n_kv_heads * max_rows = 8 (row, head) pairs per KV head are served by the kernel behind kvq_decode_attention where it
  *     is built for the configuration, some more rows over long caches by several launches of it (capacity and window tell, so a
  *     capacity far above the lengths costs such calls time), everything else by one that makes 16-bit tiles of the pages for the

@@ -74,6 +74,10 @@ int kvq_debug_paged_stall(const kvq_config* cfg, const kvq_paged_cache* cache, c
                           int32_t max_rows, int32_t window, int32_t sinks, void* out, int32_t out_dtype, void* workspace,
                           size_t workspace_bytes, int64_t skip_page, uint32_t wait_us, void* cuda_stream);
 
+/* Host only, no GPU work: launches = the launches of the decode kernel that serve such a kvq_paged_attention call, 0 where the chunk
+ * kernel serves it. */
+int kvq_debug_paged_launches(const kvq_config* cfg, int32_t max_rows, int32_t window, int32_t sinks, int32_t* launches);
+
 #ifdef __cplusplus
 }
 #endif

@@ -107,6 +107,7 @@ int launch_paged_append(const Geom& g, const Paged& p, const void* k, const void
 int launch_paged_dequantize(const Geom& g, const Paged& p, void* k_out, void* v_out, cudaStream_t stream);
 // few rows (g.rows: the most rows of a sequence), where it serves the call; bytes of workspace behind the count words for any window
 bool paged_decode_serves(const Geom& g, const Paged& p);
+int paged_decode_launches(const Geom& g, const Paged& p);      // 0 where it does not
 size_t paged_decode_workspace_bytes(const Geom& g);
 int launch_paged_decode(const Geom& g, const Paged& p, const void* q, void* out, int out_dtype, float scale_log2e, float* ws,
                         const DecodeDebug& dbg, cudaStream_t stream);

@@ -48,7 +48,7 @@ int rows_per_launch(const Geom& g, const Paged& p) {
     Geom part = g;
     part.rows = g.rows < pairs / g.G ? g.rows : pairs / g.G;
     if (part.rows < 1) continue;
-    const long long launches = (g.rows + part.rows - 1) / part.rows;
+    const long long launches = ((long long)g.rows + part.rows - 1) / part.rows;
     if (launches > 5 || (launches > 1 && launches * (9 * 1480 + 5 * pages) >= 13 * 1480 + 26 * pages)) continue;      // (26 / 5: six never win)
     if (pick_paged(part, p, nullptr, 0.f, nullptr, nullptr, 0, DecodeDebug{}, nullptr, true) == KVQ_OK) return part.rows;
   }
@@ -58,6 +58,11 @@ int rows_per_launch(const Geom& g, const Paged& p) {
 }  // namespace
 
 bool paged_decode_serves(const Geom& g, const Paged& p) { return rows_per_launch(g, p) > 0; }
+
+int paged_decode_launches(const Geom& g, const Paged& p) {
+  const int step = rows_per_launch(g, p);
+  return step > 0 ? (g.rows + step - 1) / step : 0;      // (a few: rows_per_launch sees to it)
+}
 
 size_t paged_decode_workspace_bytes(const Geom& g) {
   Geom part = g;

@@ -43,6 +43,16 @@ size_t paged_workspace_bytes(const Geom& g) {
   return count_words_bytes(g) + (decode > chunk ? decode : chunk);
 }
 
+// The most rows of a sequence that an attention call can have: max_rows may be any bound, but no sequence has more rows than tokens.
+int32_t bounded_rows(const Geom& g, int32_t max_rows) { return max_rows < g.capacity ? max_rows : g.capacity; }
+
+// What an attention call announces.
+void set_rows(Geom* g, Paged* p, int32_t max_rows, int32_t window, int32_t sinks) {
+  g->rows = p->max_rows = bounded_rows(*g, max_rows);
+  p->window = window;
+  p->sinks = sinks;
+}
+
 int attention_with(const DecodeDebug& dbg, const kvq_config* cfg, const kvq_paged_cache* cache, const void* q, const int32_t* cu, int32_t n_rows,
                    int32_t max_rows, int32_t window, int32_t sinks, void* out, int32_t out_dtype, float softmax_scale,
                    void* workspace, size_t workspace_bytes, void* cuda_stream) {
@@ -56,10 +66,7 @@ int attention_with(const DecodeDebug& dbg, const kvq_config* cfg, const kvq_page
   if (!q || !out || !workspace) return KVQ_ERR_INVALID_ARG;
   if (out_dtype != KVQ_FP16 && out_dtype != KVQ_BF16 && out_dtype != KVQ_FP32) return KVQ_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return KVQ_ERR_MISALIGNED;
-  g.rows = max_rows;
-  p.max_rows = max_rows;
-  p.window = window;
-  p.sinks = sinks;
+  set_rows(&g, &p, max_rows, window, sinks);
   if (workspace_bytes < paged_workspace_bytes(g)) return KVQ_ERR_WORKSPACE_TOO_SMALL;
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)g.D);
   const float c1 = scale * 1.4426950408889634f;
@@ -106,7 +113,7 @@ int kvq_paged_workspace_bytes(const kvq_config* cfg, int32_t max_rows, size_t* o
   const int rc = paged_geom(cfg, &g);
   if (rc != KVQ_OK) return rc;
   if (!out || max_rows < 1) return KVQ_ERR_INVALID_ARG;
-  g.rows = max_rows;
+  g.rows = bounded_rows(g, max_rows);
   *out = paged_workspace_bytes(g);
   return KVQ_OK;
 }
@@ -127,6 +134,17 @@ int kvq_debug_paged_stall(const kvq_config* cfg, const kvq_paged_cache* cache, c
   dbg.wait_us = wait_us;
   return attention_with(dbg, cfg, cache, q, cu, n_rows, max_rows, window, sinks, out, out_dtype, 0.0f, workspace, workspace_bytes,
                         cuda_stream);
+}
+
+int kvq_debug_paged_launches(const kvq_config* cfg, int32_t max_rows, int32_t window, int32_t sinks, int32_t* launches) {
+  Geom g;
+  const int rc = paged_geom(cfg, &g);
+  if (rc != KVQ_OK) return rc;
+  if (!launches || max_rows < 1 || window < 0 || sinks < 0) return KVQ_ERR_INVALID_ARG;
+  Paged p{};
+  set_rows(&g, &p, max_rows, window, sinks);
+  *launches = paged_decode_launches(g, p);
+  return KVQ_OK;
 }
 
 int kvq_paged_dequantize(const kvq_config* cfg, const kvq_paged_cache* cache, const int32_t* cu, int32_t n_rows, void* k_out,

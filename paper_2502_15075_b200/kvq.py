@@ -95,6 +95,7 @@ _lib.kvq_paged_dequantize.argtypes = [_P(kvq_config), _P(kvq_paged_cache), ctype
                                       ctypes.c_void_p, ctypes.c_void_p]
 _lib.kvq_debug_paged_stall.argtypes = [_P(kvq_config), _P(kvq_paged_cache), ctypes.c_void_p, ctypes.c_void_p] + [ctypes.c_int32] * 4 + [
     ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64, ctypes.c_uint32, ctypes.c_void_p]
+_lib.kvq_debug_paged_launches.argtypes = [_P(kvq_config)] + [ctypes.c_int32] * 3 + [_P(ctypes.c_int32)]
 _lib.kvq_paged_check_status.argtypes = [_P(kvq_paged_cache), ctypes.c_void_p]
 _lib.kvq_check_status.argtypes = [_P(kvq_cache), ctypes.c_void_p]
 _lib.kvq_strerror.argtypes = [ctypes.c_int]
@@ -104,7 +105,8 @@ for _f in ("kvq_page_bytes", "kvq_cache_bytes", "kvq_workspace_bytes", "kvq_quan
            "kvq_quant_error", "kvq_bit_balance", "kvq_debug_decode_generic", "kvq_debug_decode_stall",
            "kvq_debug_decode_impl", "kvq_debug_decode_stall_impl", "kvq_debug_decode_plan", "kvq_debug_decode_ring", "kvq_debug_decode_windows",
            "kvq_debug_divide", "kvq_workspace_bytes_rows", "kvq_decode_attention_rows", "kvq_paged_append", "kvq_paged_workspace_bytes",
-           "kvq_paged_attention", "kvq_paged_dequantize", "kvq_paged_check_status", "kvq_debug_paged_stall"):
+           "kvq_paged_attention", "kvq_paged_dequantize", "kvq_paged_check_status", "kvq_debug_paged_stall",
+           "kvq_debug_paged_launches"):
     getattr(_lib, _f).restype = ctypes.c_int
 
 EXPORTS = ("kvq_layout_version", "kvq_page_bytes", "kvq_cache_bytes", "kvq_workspace_bytes",
@@ -530,6 +532,14 @@ def kvq_debug_paged_stall(cfg: kvq_config, cache: PagedCache, q: torch.Tensor, c
                                       out.data_ptr(), _dtype_code(out.dtype), workspace.data_ptr(),
                                       workspace.numel() * workspace.element_size(), int(skip_page), int(wait_us), _stream_ptr(None)),
            "kvq_debug_paged_stall")
+
+
+def kvq_debug_paged_launches(cfg: kvq_config, max_rows: int, window: int = 0, sinks: int = 0) -> int:
+    """Test hook, host only: launches of the decode kernel for such an attention call, 0 where the chunk kernel serves it."""
+    out = ctypes.c_int32()
+    _check(_lib.kvq_debug_paged_launches(ctypes.byref(cfg), int(max_rows), int(window), int(sinks), ctypes.byref(out)),
+           "kvq_debug_paged_launches")
+    return out.value
 
 
 def kvq_paged_dequantize(cfg: kvq_config, cache: PagedCache, cu: torch.Tensor, k_out: Optional[torch.Tensor],
