@@ -43,7 +43,10 @@ int pick_paged(const Geom& g, const Paged& p, const void* q, float c1, float* ws
 // known here: the capacity and the window stand for them.
 int rows_per_launch(const Geom& g, const Paged& p) {
   const long long tokens = p.window > 0 && (long long)p.window + p.sinks < g.capacity ? (long long)p.window + p.sinks : g.capacity;
-  const long long pages = ((tokens + kPageTokens - 1) / kPageTokens + (tokens < g.capacity)) * g.B * g.Hkv;
+  const long long per_stream = (tokens + kPageTokens - 1) / kPageTokens + (tokens < g.capacity), pages = per_stream * g.B * g.Hkv;
+  // (its prefixes over the batch are 32 bits; sequences may share pool pages, so memory does not bound them.  24: a stream's gap, and the
+  // pages at a window's and the first tokens' ends)
+  if ((per_stream + 24) * g.B * g.Hkv > 0x7FFFFFFFll) return 0;
   for (int pairs = kMaxGroupHeads; pairs >= 4; pairs -= 4) {
     Geom part = g;
     part.rows = g.rows < pairs / g.G ? g.rows : pairs / g.G;

@@ -41,3 +41,16 @@ def test_single_tokens_and_prompts(kvq):
     assert kvq.kvq_debug_paged_launches(cfg, 1) == 1
     assert kvq.kvq_debug_paged_launches(cfg, 2) == 1
     assert kvq.kvq_debug_paged_launches(cfg, 8192) == 0
+
+
+@pytest.mark.parametrize("batch,kv_heads,capacity,few", [
+    (1024, 8, 131072, True), (1024, 63, 4 << 20, True), (1024, 63, 8 << 20, False), (1024, 8, 2 ** 31 - 128, False), (1, 8, 2 ** 31 - 128, True)])
+def test_pages_that_pass_31_bits_go_to_the_kernel_that_counts_in_64(kvq, batch, kv_heads, capacity, few):
+    """Pool pages may be shared by sequences, so the pages that a batch sees are not bounded by memory: the decode kernel's prefixes are
+    32-bit numbers of pages (and up to 18 more per stream), the other kernel's 64-bit ones."""
+    cfg = cfg_of(kvq, batch=batch, n_q_heads=kv_heads, n_kv_heads=kv_heads, capacity_tokens=capacity)
+    assert few == (batch * kv_heads * (capacity // 128 + 18) < 2 ** 31)
+    for rows in (1, 8):
+        for window in (0, LAST):
+            assert (kvq.kvq_debug_paged_launches(cfg, rows, window) > 0) == few
+    assert kvq.kvq_debug_paged_launches(cfg, 1, 1000, 4) > 0          # a window's pages are few
