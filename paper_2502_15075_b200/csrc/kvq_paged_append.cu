@@ -42,7 +42,7 @@ __device__ __forceinline__ uint32_t pack16(float a, float b) {
 }
 
 // A lane's part of a position's rows of the table: cos, sin of its eight channels' pairs (of four pairs, twice, where interleaved); where
-// halves are paired the sine carries the sign of the channel's half.  Channels from rotary_dim on get (1, +0).
+// halves are paired the sine carries the sign of the channel's half.  Channels from rotary_dim on get (1, 0), which nobody uses.
 template <int D>
 __device__ __forceinline__ void load_angles(const RopeArgs& r, int t, int l, float (&c)[8], float (&s)[8]) {
 #pragma unroll
@@ -61,7 +61,7 @@ __device__ __forceinline__ void load_angles(const RopeArgs& r, int t, int l, flo
 }
 
 // Rotation of a row, lane l of its D / 8 lanes holding channels 8 l .. 8 l + 7.  All lanes of the warp take part.  A channel that is not
-// turned is its own partner: x 1 + x (+0) = x, to the sign of a zero.
+// turned is its own partner and stays as it is (x 1 + x (+0) would make an infinity NaN).
 template <int D>
 __device__ __forceinline__ void rotate_row(float (&x)[8], const RopeArgs& r, const float (&c)[8], const float (&s)[8], int l) {
   const int lh = r.half >> 3;
@@ -80,7 +80,8 @@ __device__ __forceinline__ void rotate_row(float (&x)[8], const RopeArgs& r, con
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float o = __shfl_sync(FULL, x[i], partner, D / 8);
-      x[i] = __fadd_rn(__fmul_rn(x[i], c[i]), __fmul_rn(o, s[i]));
+      const float y = __fadd_rn(__fmul_rn(x[i], c[i]), __fmul_rn(o, s[i]));
+      x[i] = turned ? y : x[i];
     }
   }
 }
