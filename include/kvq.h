@@ -266,11 +266,14 @@ int kvq_bit_balance(double sum_k2, double sum_v2, double* bk_minus_bv);
  * holds once the call's tokens are counted in: row i stands at position seq_len[b] - cu[b + 1] + i.  The library never changes
  * seq_len, so that all layers share one.  Rows from cu[batch] on are padding (a captured graph's) and are left as they were.
  *
- * Everything in device memory is checked before it is used as an index.  A sequence with decreasing or too large offsets, more
- * rows than tokens, a length beyond capacity_tokens (or the rotation's table, or with more than max_rows rows) is passed
- * over: none of its rows is written.  A page number outside the pool makes the append leave out the tokens of that page, the read-back
+ * Everything in device memory is checked before it is used as an index.  A sequence with more rows than tokens, a length that is negative or
+ * beyond capacity_tokens (or the rotation's table, or with more than max_rows rows) is passed over: none of its rows is written.  Where the
+ * offsets are out of order (negative, decreasing or beyond n_rows), the attention passes over the sequences between such offsets; which of the
+ * call's tokens the append then stores (a token's keys may come without its values) and which rows the read-back fills is undefined, the tokens in
+ * front of the call's stay.  A page number outside the pool makes the append leave out the tokens of that page, the read-back
  * leave their rows as they were, and the attention's rows of that sequence undefined (another page is read in its place).  All
- * of these set KVQ_STATUS_BAD_INPUT.  Different tokens of a call have to lie in different places; all calls are asynchronous on cuda_stream.
+ * of these set KVQ_STATUS_BAD_INPUT, a bad length also where the sequence has no rows in the call.  Different tokens of a call have to lie in
+ * different places; all calls are asynchronous on cuda_stream.
  * ------------------------------------------------------------------------------------------------------------------- */
 typedef struct {
   void* pages;                /* device; 16-byte aligned; pool as above */

@@ -32,13 +32,23 @@ __device__ __forceinline__ SeqRows seq_rows(const Paged& p, int b, int limit, in
   return SeqRows{bad ? 0 : n, bad ? 0 : c1 - c0, bad ? 0 : c0};
 }
 
-// Its rows from .. from + most - 1 alone: as a call of just these tokens.
+// Says what is out of range in a call (one warp of it), of sequences without rows too: those are nobody's task.
+__device__ __forceinline__ void report_bad_input(const Paged& p, int B, int limit, int lane) {
+  for (int b = lane; b < B; b += 32) {
+    bool bad;
+    seq_rows(p, b, limit, p.n_rows, bad);
+    if (bad) atomicOr(p.status, KVQ_STATUS_BAD_INPUT);
+  }
+}
+
+// Rows from .. from + most - 1 of a sequence alone: as a call of just these tokens.
 __device__ __forceinline__ SeqRows part_of(const SeqRows& s, int from, int most) {
   const int rows = min(max(s.rows - from, 0), most);
   return SeqRows{rows > 0 ? s.n - (s.rows - from - rows) : s.n, rows, s.first + from};
 }
 
-// The sequence of row i: the number of ends cu[1 ..] at or below it.  The whole warp asks for the same row.
+// The sequence of row i: the number of ends cu[1 ..] at or below it.  The whole warp asks for the same row.  (Offsets out of order lead to some
+// sequence, here and by blocks below; looking at all of them first costs appends and read-backs 3 %.)
 __device__ __forceinline__ int sequence_of(const int32_t* cu, int B, int i, int lane) {
   int lo = 0, len = B;                           // the answer is in lo .. lo + len - 1 (or B, which the caller's check finds out)
   while (len > 32) {
@@ -69,7 +79,6 @@ __device__ __forceinline__ BlockTask block_task(const Paged& p, int B, int slot,
   }
   bool bad;
   const SeqRows s = seq_rows(p, lo, limit, max_rows, bad);
-  if (bad && lane == 0) atomicOr(p.status, KVQ_STATUS_BAD_INPUT);
   BlockTask t{lo, 0, 0, 0, 0};
   if (s.rows == 0) return t;
   const int start = s.n - s.rows, skipped = slot - (s.first / span + 2 * lo);

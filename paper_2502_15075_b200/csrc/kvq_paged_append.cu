@@ -119,7 +119,7 @@ paged_append_rows_kernel(Geom g, Paged p, AppendArgs a, int per_token, int group
   bool bad;
   const int limit = a.rope.half ? min(g.capacity, a.rope.n_positions) : g.capacity;
   const SeqRows s = seq_rows(p, b, limit, p.n_rows, bad);
-  if (bad && lane == 0) atomicOr(p.status, KVQ_STATUS_BAD_INPUT);
+  if (task == 0) report_bad_input(p, g.B, limit, lane);
   if (row < s.first || row >= s.first + s.rows) return;
   const int t = s.n - s.rows + (row - s.first);
   const int id = pool_page(p, b, t >> 7);

@@ -131,6 +131,7 @@ paged_dequant_kernel(Geom g, Paged p, uint16_t* k_out, uint16_t* v_out, int firs
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   long long task = (long long)blockIdx.x * kWarps + warp;
   begin_after_predecessor();
+  if (task == 0) report_bad_input(p, g.B, g.capacity, lane);
   const int side = first_side + (int)(task % sides);
   task /= sides;
   const int h = (int)(task % g.Hkv);
