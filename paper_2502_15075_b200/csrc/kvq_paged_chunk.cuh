@@ -13,7 +13,9 @@
 //    sums in fp32.  While one half's softmax runs, the tensor cores have the other half's products.  The reference moves only when a logit
 //    passes it by kHeadroom bits; then the row's outputs are rescaled in tensor memory.
 // The order of the fp16 weights' rounding (2^-11 of a weight at most) and of the tiles' is the loss against fp32; all sums are fp32.
-// bf16 queries are scaled by a power of two per row, pages whose values pass half the fp16 range by 2^-10 (undone in fp32 and in P).
+// bf16 queries are scaled by a power of two per row.  A token with a group that reaches beyond the fp16 range enters its tile times 2^-(B + 1), which
+// brings the largest B-bit group into it; its logit (keys) or its weight (values) is made as much larger.  Other tokens of its page are as exact as
+// without it.
 //
 // The (tile, page) pairs of a call lie on one axis that is cut into equal shares, one per CTA, so that a long prompt, a ragged batch and a few
 // drafted rows behind a long context all fill the GPU.  A tile that falls to several CTAs leaves partials (m, l, o); the CTA that comes last
@@ -27,6 +29,8 @@
 // Every wait is bounded; on expiry the kernel sets KVQ_STATUS_DEVICE_TIMEOUT, goes on without waiting (nothing that it then reads is out of range) and
 // frees its tensor memory.
 #pragma once
+
+#include <type_traits>
 
 #include "kvq_paged.cuh"
 #include "kvq_tcgen05.cuh"
@@ -46,7 +50,7 @@ constexpr int kTile = 256;                 // (query row, head) pairs of a tile
 // 6 746; the chunks 156, 157, 160, 157.
 constexpr int kGap = 5;
 constexpr float kHeadroom = 4.0f;
-constexpr float kBigDown = 9.765625e-4f, kBigUp = 1024.0f;      // 2^-10 for pages whose values pass half the fp16 range, and back
+__host__ __device__ constexpr float big_up(int bits) { return (float)(2 << bits); }      // of tokens beyond the fp16 range, see above
 constexpr uint32_t FULL = 0xffffffffu;
 // tensor memory: S of the two halves (columns 0-31 and 64-95 of each take P), then O of the two halves
 constexpr uint32_t kColS = 0, kColO = 256, kTmemCols = 512;
@@ -69,7 +73,7 @@ __host__ __device__ inline Smem smem_of(int batch) {
   s.v = s.k + 2 * T::kK;
   s.bars = s.v + 2 * T::kV;
   s.misc = s.bars + 32 * 8;
-  s.rows = s.misc + 64;                      // per row of the tile: what its two threads tell each other, for two pages in turn
+  s.rows = s.misc + 160;                     // per row of the tile: what its two threads tell each other, for two pages in turn
   s.pref = s.rows + 2 * kTile * 2 * 4;
   s.seq = s.pref + (batch + 1) * 8;
   s.total = s.seq + 3 * batch * 4;
@@ -123,6 +127,15 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]
 __device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&r)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr), KVQ_S8(r, 0) : "memory");
 }
+// One column, there at once.
+__device__ __forceinline__ uint32_t tmem_ld1(uint32_t addr) {
+  uint32_t r;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(r) : "r"(addr) : "memory");
+  return r;
+}
+__device__ __forceinline__ void tmem_st1(uint32_t addr, uint32_t r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(addr), "r"(r) : "memory");
+}
 __device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t sel) {
   uint32_t d;
   asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(sel));
@@ -133,16 +146,26 @@ __device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
   return d;
 }
-__device__ __forceinline__ bool bar_any(int id, int nthreads, bool p) {
-  uint32_t r;
-  __syncwarp();
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(r) : "r"((uint32_t)p), "r"(id), "r"(nthreads) : "memory");
-  return r != 0;
-}
-
 // Token of a page's block of 32 that stands at place k of its 32 columns: codes of four tokens share a word, those of two halves a load.
 __host__ __device__ constexpr int token_at(int k) { return 16 * ((k & 7) >> 2) + 2 * (k >> 3) + (k & 1) + 8 * ((k >> 1) & 1); }
+
+// Its inverse: the place of token u.
+__host__ __device__ constexpr int place_of(int u) { return 8 * ((u & 7) >> 1) + (u & 1) + 2 * ((u >> 3) & 1) + 4 * (u >> 4); }
+constexpr bool places_match() {
+  for (int k = 0; k < 32; ++k)
+    if (place_of(token_at(k)) != k) return false;
+  return true;
+}
+static_assert(places_match(), "columns of single tokens");
+// Of the tokens marked in two blocks' words (the same for the whole warp): what to do with each one's column.
+template <typename F>
+__device__ __forceinline__ void for_tokens(uint32_t first, uint32_t second, F&& each) {
+#pragma unroll 1
+  for (int base = 0; base < 64; base += 32) {
+#pragma unroll 1
+    for (uint32_t bits = base == 0 ? first : second; bits; bits &= bits - 1) each(base + place_of(__ffs(bits) - 1));
+  }
+}
 
 // Two codes of a field of a word's bytes 0 and 2 (of w >> 8: bytes 1 and 3) as fp16 numbers times scale plus zero-point, one rounding.  The
 // field stays where it stands: under the bits of 1024 it reads 1024 + code 2^(B f), which one operation makes the code, exactly.
@@ -187,9 +210,18 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
   const Smem sl = smem_of<D>(g.B);
   long long* sPref = reinterpret_cast<long long*>(smem + sl.pref);      // (tile, page) pairs and gaps in front of every sequence
   int* sSeq = reinterpret_cast<int*>(smem + sl.seq);                    // tokens, rows, first row
-  int* sMisc = reinterpret_cast<int*>(smem + sl.misc);                  // [0] abort [1] tensor memory [2, 3] counts returned [4..7] share [8..11] pages of big keys [12..15] ... of big values
+  int* sMisc = reinterpret_cast<int*>(smem + sl.misc);                  // [0] abort [1] tensor memory [2, 3] counts returned [4..7] share [8..39] tokens that are scaled
   volatile int* abort_flag = sMisc;
-  volatile int* sBig = sMisc + 8;           // by page: keys, then values
+  // which tokens are scaled: a bit per token; four pages in turn, two sides of 64 tokens, their two blocks' keys, then values
+  const uint32_t sScaled = smem_u32(sMisc + 8);
+  auto get_scaled = [&](int it, int side) {
+    uint4 b;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(sScaled + 16 * (2 * (it & 3) + side)) : "memory");
+    return b;
+  };
+  auto set_scaled = [&](int it, int blk, int of_values, uint32_t bits) {
+    asm volatile("st.shared.u32 [%0], %1;" ::"r"(sScaled + 16 * (2 * (it & 3) + (blk >> 1)) + 8 * of_values + 4 * (blk & 1)), "r"(bits) : "memory");
+  };
   const int tid_ = threadIdx.x, lane = tid_ & 31, warp = __shfl_sync(FULL, tid_ >> 5, 0);
   const int B = g.B, G = g.G, Hkv = g.Hkv;
   const uint32_t inv_g = G > 1 ? 0xFFFFFFFFu / (uint32_t)G + 1u : 0u;
@@ -441,13 +473,10 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       const int lim_all = t.n - t.rows + r_first + 1, low_all = p.window > 0 ? max(t.n - t.rows + r_last + 1 - p.window, 0) : 0;
       float m = -INFINITY;
       f32x2 l2 = pack2(0.f, 0.f);
-#pragma unroll 1
-      for (int j = 0; j < pages; ++j, ++it, ++done) {
-        wait_warp(bS + 8 * w, done & 1);
-        tc::tc_fence_after();
-        wait_warp(bVF + 8 * (it & 1), (it >> 1) & 1);          // (there by now: the values' tile and whether it is scaled)
-        const bool big = sBig[4 + (it & 3)] != 0;
-        const float fs = sBig[it & 3] != 0 ? f * kBigUp : f;
+      int j = 0;
+      // Page j: S to weights.  SCALED: of this side's tokens some are scaled.
+      auto soften = [&](auto scaled_tag) {
+        constexpr bool SCALED = decltype(scaled_tag)::value;
         const int tok = t.seen.logical(page0 + j) * kPageTokens;
         const bool open = tok + kPageTokens <= lim_all && (tok >= low_all || tok + kPageTokens <= p.sinks);       // every row sees the whole page
         const int lim_t = lim - tok, low_t = low - tok, sink_t = p.sinks - tok;
@@ -472,6 +501,16 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
           tc::tc_wait_st();
         }
         float top = -INFINITY;
+        [[maybe_unused]] float top_big = -INFINITY;
+        if constexpr (SCALED) {
+          // logits of tokens whose keys are scaled: as much larger; what those count whose values are scaled (their weights have to fit too)
+          const uint4 b = get_scaled(it, side);
+          for_tokens(b.x, b.y, [&](int column) {
+            tmem_st1(tS + column, __float_as_uint(__uint_as_float(tmem_ld1(tS + column)) * big_up(KB)));
+            tc::tc_wait_st();
+          });
+          for_tokens(b.z, b.w, [&](int column) { top_big = fmaxf(top_big, fmaf(__uint_as_float(tmem_ld1(tS + column)), f, (float)(VB + 1))); });
+        }
 #pragma unroll 1
         for (int c = 0; c < 64; c += 16) {
           tmem_ld16(tS + c, a);
@@ -481,8 +520,9 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
           for (int k = 5; k < 13; k += 4) { t0 = max3(t0, a[k], a[k + 1]); t1 = max3(t1, a[k + 2], a[k + 3]); }
           top = max3(max3(t0, a[13], a[14]), __float_as_uint(t1), a[15]);
         }
+        top *= f;
+        if constexpr (SCALED) top = fmaxf(top, top_big);
         top = fmaxf(top, exchange(top));
-        top *= fs;
         // ---- the reference moves when a logit passes it by the headroom
         const bool move = top > m + kHeadroom;       // (m = -inf: any logit at all)
         if (__any_sync(FULL, move)) {
@@ -502,9 +542,9 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
           l2 = mul2(l2, pack2(keep, keep));
           m = nm;
         }
-        // ---- weights: 2^(x - m), fp16, where S was (columns that this warp has read); pages of big values carry P times 2^10
-        const float base = (m == -INFINITY ? 0.f : m) - (big ? 10.0f : 0.0f);
-        const f32x2 f2 = pack2(fs, fs), nb = pack2(-base, -base);
+        // ---- weights: 2^(x - m), fp16, where S was (columns that this warp has read)
+        const float base = m == -INFINITY ? 0.f : m;
+        const f32x2 f2 = pack2(f, f), nb = pack2(-base, -base);
         f32x2 sum = pack2(0.f, 0.f);
         auto weigh = [&](const uint32_t (&s)[16], uint32_t to) {
           uint32_t w16[8];
@@ -523,13 +563,39 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
           wait_ld(a);
           weigh(a, tS + (c >> 1));
         }
-        const float back = big ? kBigDown : 1.0f;
-        l2 = fma2(sum, pack2(back, back), l2);
+        l2 = add2(l2, sum);
+        if constexpr (SCALED) {
+          // weights of tokens whose values are scaled: as much larger
+          tc::tc_wait_st();
+          const uint4 b = get_scaled(it, side);
+          for_tokens(b.z, b.w, [&](int column) {
+            const uint32_t at = tS + (column >> 1), both = tmem_ld1(at), up = as_u32(__float2half2_rn(big_up(VB)));
+            tmem_st1(at, as_u32(__hmul2(as_h2(both), as_h2(column & 1 ? (up & 0xFFFF0000u) | 0x3C00u : (up & 0xFFFFu) | 0x3C000000u))));
+            tc::tc_wait_st();
+          });
+        }
         tc::tc_wait_st();
         tc::tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bP + 8 * w);
+        ++j; ++it; ++done;
+      };
+      // (pages with scaled tokens leave the loop over the others: within it their code, never reached, made the prompt 2 to 4 % slower)
+#pragma unroll 1
+      while (true) {
+#pragma unroll 1
+        while (true) {
+          if (j == pages) goto pages_done;
+          wait_warp(bS + 8 * w, done & 1);
+          tc::tc_fence_after();
+          wait_warp(bVF + 8 * (it & 1), (it >> 1) & 1);          // (there by now: the values' tile and what of it is scaled)
+          const uint4 b = get_scaled(it, side);
+          if (__any_sync(FULL, (b.x | b.y | b.z | b.w) != 0)) break;
+          soften(std::false_type{});
+        }
+        soften(std::true_type{});
       }
+    pages_done:
       // ---- the tile's outputs, or its partial
       wait_warp(bO + 8 * w, seg & 1);
       ++seg;
@@ -696,7 +762,7 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
     };
     look_up();
     // Scales and zero-points of the lane's token, a word per group; nothing of tokens that the sequence does not hold (their bytes are
-    // anything).  True where a value may pass half the fp16 range.
+    // anything).  True where a value may pass the fp16 range (zero-points are in it).
     auto load_meta = [&](uint32_t (&m)[4], int off, int count) {
       const uint32_t* src = reinterpret_cast<const uint32_t*>(page_ptr + off) + (32 * blk + lane) * count;
 #pragma unroll
@@ -709,14 +775,14 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
         if (e < count) {
           if (!there) m[e] = 0u;
           const float2 sz = __half22float2(as_h2(m[e]));
-          wide |= fabsf(sz.y) > 32752.0f || sz.x * qmax > 32752.0f;
+          wide |= fmaf(sz.x, qmax, sz.y) > 65504.0f;
         }
       }
       return wide;
     };
-    auto scale_meta = [&](uint32_t (&m)[4], int count) {
+    auto scale_meta = [&](uint32_t (&m)[4], int count, float down) {
 #pragma unroll
-      for (int e = 0; e < NI; ++e) if (e < count) m[e] = as_u32(__hmul2(as_h2(m[e]), __float2half2_rn(kBigDown)));
+      for (int e = 0; e < NI; ++e) if (e < count) m[e] = as_u32(__hmul2(as_h2(m[e]), __float2half2_rn(down)));
     };
     int it = 0;
     if (warp < 24) {
@@ -737,10 +803,11 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       for (; more; ++it) {
           const int buf = it & 1;
           const bool there = lane < tokens;
-          const bool wide = check_meta(km, ngk, (float)((1 << KB) - 1), there), big = bar_any(3, 256, wide);
-          if (big) scale_meta(km, ngk);
+          const bool wide = check_meta(km, ngk, (float)((1 << KB) - 1), there);
+          if (wide) scale_meta(km, ngk, 1.0f / big_up(KB));
+          const uint32_t big = __ballot_sync(FULL, wide);
           if (it >= 2) wait_warp(bKE + 8 * buf, ((it >> 1) - 1) & 1);
-          if (warp == 16 && lane == 0) sBig[it & 3] = big;
+          if (half == 0 && lane == 0) set_scaled(it, blk, 0, big);
           uint8_t* dst = smem + sl.k + buf * T::kK;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
@@ -787,10 +854,10 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
           const int buf = it & 1;
           const bool there = lane < tokens;
           const bool wide = check_meta(vm, ngv, (float)((1 << VB) - 1), there);
-          const bool big = bar_any(4, 128, wide);
-          if (big) scale_meta(vm, ngv);
+          if (wide) scale_meta(vm, ngv, 1.0f / big_up(VB));
+          const uint32_t big = __ballot_sync(FULL, wide);
           if (it >= 2) wait_warp(bVE + 8 * buf, ((it >> 1) - 1) & 1);
-          if (warp == 24 && lane == 0) sBig[4 + (it & 3)] = big;
+          if (lane == 0) set_scaled(it, blk, 1, big);
           uint8_t* dst = smem + sl.v + buf * T::kV + vl * 16 + (4 * blk + tq) * T::kLbV;
           __half2 s[2][2], z[2][2];                  // [half][pair of tokens]
 #pragma unroll

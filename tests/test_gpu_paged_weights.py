@@ -1,0 +1,86 @@
+"""Paged attention of many rows where 16-bit tiles and weights are at the end of their range: flat tails under peaks, values beside
+much larger ones.  References: fp64 NumPy on the same packed bytes."""
+import numpy as np
+import pytest
+import torch
+
+import paged_testlib as pt
+
+pytestmark = pytest.mark.gpu
+
+S = pt.Shape
+
+
+@pytest.fixture(scope="module")
+def kvq():
+    from paper_2502_15075_b200 import build
+    build.build()
+    from paper_2502_15075_b200 import kvq as mod
+    return mod
+
+
+def refill(call, make):
+    """Store rows make(sequence, tokens) -> (k, v) [tokens, Hkv, D] over all tokens of a call's sequences."""
+    for b, n in enumerate(call.lens):
+        where = [(int(call.table[b, t // 128]), t % 128) for t in range(n)]
+        keep = [i for i, (p, _) in enumerate(where) if p >= 0]
+        k, v = make(b, n)
+        pt.store(call.pages, call.sh, [where[i] for i in keep], k[keep].astype(np.float32), v[keep].astype(np.float32))
+
+
+@pytest.mark.parametrize("side", ["keys", "values"])
+@pytest.mark.parametrize("sh", [S(), S(kb=8, vb=8), S(kb=2, vb=4, gk=32, gv=64), S(D=64, kb=4, vb=8, gk=64, gv=32)], ids=str)
+def test_small_values_beside_a_large_one(kvq, sh, side):
+    """A token beyond half the fp16 range in a page of small ones: rows that do not see it (earlier ones, or behind the window) are served
+    as exactly as without it."""
+    rng = np.random.default_rng(2)
+    for n, rows, window, at in ((300, 200, 0, 250), (700, 400, 100, 300)):
+        call = pt.Call(kvq, sh, [n], [rows], window, 0, seed=3)
+        small = 1e-3
+
+        def make(_, n):
+            k, v = (rng.standard_normal((n, sh.Hkv, sh.D)) for _ in range(2))
+            x = k if side == "keys" else v
+            x *= np.where(np.arange(n) == at, 4e4, small)[:, None, None]
+            return k, v
+        refill(call, make)
+        if side == "keys":
+            call.q = (call.q.float() / small).to(call.q.dtype)
+        got, want = call.got_attention(), call.want_attention()
+        assert np.all(np.isfinite(got))
+        p = np.arange(n - rows, n)
+        blind = (p < at) | ((p - window >= at) if window else False)
+        # K^, V^ and the weights are off by 2^-11 of themselves; an error of K^ moves a logit of deviation one by 2^-11, a weight's ratio to
+        # the others by sqrt(2) as much at most: (1 + 1 + sqrt 2) 2^-11 = 1.7e-3 where nothing averages out
+        rel = np.linalg.norm(got - want, axis=-1) / np.linalg.norm(want, axis=-1)
+        assert blind.sum() > 100 and rel[blind].max() <= 2e-3, f"rows that do not see the large token: {rel[blind].max():.2e}"
+        if side == "keys":
+            # Rows that see the large key have logits of up to 1e8 there, off by 2^-11 of the products' sum at most: which side of the others such a
+            # logit lies on is only known beyond that.  (32: bits in fp32 beyond which a weight is nothing, twice the others' logits)
+            K, _ = zip(*(pt.gather(call.pages, sh, call.table[0], n, h) for h in range(sh.Hkv)))
+            k = np.repeat(np.stack([x[at] for x in K]), sh.G, axis=0)
+            terms = call.q.double().numpy() * k / np.sqrt(sh.D)
+            known = np.abs(terms.sum(-1)) > 2.0 ** -11 * np.abs(terms).sum(-1) + 32
+            known[blind] = True
+            assert known[~blind].mean() > 0.9 if (~blind).any() else True
+            got, want = got[known], want[known]
+        assert np.linalg.norm(got - want) / np.linalg.norm(want) <= 2e-3
+
+
+@pytest.mark.parametrize("sh", [S(), S(kb=8, vb=8), S(kb=2, vb=2, dtype="bf16")], ids=str)
+def test_the_largest_values_a_page_can_hold(kvq, sh):
+    """Groups from -65504 on with the largest scale: up to 2^24, in several tokens of a page and in whole pages."""
+    rng = np.random.default_rng(4)
+    n, rows = 500, 150
+    call = pt.Call(kvq, sh, [n], [rows], seed=5)
+    t = np.arange(n)
+    top = 65504.0 * 2 ** sh.vb
+
+    def make(_, n):
+        k, v = (rng.standard_normal((n, sh.Hkv, sh.D)) for _ in range(2))
+        v *= np.where((t % 41 == 3) | (t // 128 == 1), top / 4, 1.0)[:, None, None]
+        return k, np.clip(v, -6e4, top)
+    refill(call, make)
+    got, want = call.got_attention(), call.want_attention()
+    assert np.all(np.isfinite(got))
+    assert np.linalg.norm(got - want) / np.linalg.norm(want) <= 2e-3
