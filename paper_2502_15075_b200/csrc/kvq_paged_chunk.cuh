@@ -11,8 +11,8 @@
 //    in turn, and O += P V with P read from tensor memory, where it takes the place of S.
 //  * warps 0-7 and 8-15 take the two halves, two threads per row: row maximum, p = 2^(x - reference), fp16 weights back to tensor memory;
 //    sums in fp32.  While one half's softmax runs, the tensor cores have the other half's products.  The reference moves only when a logit
-//    passes it by kHeadroom bits; then the row's outputs are rescaled in tensor memory.
-// The order of the fp16 weights' rounding (2^-11 of a weight at most) and of the tiles' is the loss against fp32; all sums are fp32.
+//    passes the largest one before by kHeadroom bits; then the row's outputs are rescaled in tensor memory.
+// The loss against fp32 is the rounding of the weights (see kLift) and of the tiles (2^-11 of an element) to fp16; all sums are fp32.
 // bf16 queries are scaled by a power of two per row.  A token with a group that reaches beyond the fp16 range enters its tile times 2^-(B + 1), which
 // brings the largest B-bit group into it; its logit (keys) or its weight (values) is made as much larger.  Other tokens of its page are as exact as
 // without it.
@@ -49,7 +49,12 @@ constexpr int kTile = 256;                 // (query row, head) pairs of a tile
 // What a tile costs besides its pages (queries, a first product that nothing overlaps, outputs), in pages: the prompt above with 2 870 us, 3 788, 4 749,
 // 6 746; the chunks 156, 157, 160, 157.
 constexpr int kGap = 5;
-constexpr float kHeadroom = 4.0f;
+// Weights are 2^(logit - reference), the reference `lift` bits below the largest logit when it moves; it moves when a logit passes it by lift +
+// kHeadroom.  So the largest weight of a row is between 2^11 and 2^15, and a weight is off by 2^-11 of it or, below 2^-14 in fp16, by 2^-36 of the
+// largest (131,072 tokens of that kind: 2^-19).  Of logits x of millions of bits fp32 rounds x and the reference by up to 2^-24 x each: the
+// lift leaves room for that.
+constexpr float kHeadroom = 4.0f, kLift = 11.0f;
+__device__ __forceinline__ float lift_at(float x) { return fmaxf(fmaf(fabsf(x), -2.3841858e-7f, kLift), 0.0f); }      // kLift - |x| 2^-22
 __host__ __device__ constexpr float big_up(int bits) { return (float)(2 << bits); }      // of tokens beyond the fp16 range, see above
 constexpr uint32_t FULL = 0xffffffffu;
 // tensor memory: S of the two halves (columns 0-31 and 64-95 of each take P), then O of the two halves
@@ -524,9 +529,9 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
         if constexpr (SCALED) top = fmaxf(top, top_big);
         top = fmaxf(top, exchange(top));
         // ---- the reference moves when a logit passes it by the headroom
-        const bool move = top > m + kHeadroom;       // (m = -inf: any logit at all)
+        const bool move = top > m + (lift_at(m) + kHeadroom);       // (m = -inf: any logit at all)
         if (__any_sync(FULL, move)) {
-          const float nm = move ? top : m;
+          const float nm = move ? top - lift_at(top) : m;
           const float keep = m == -INFINITY ? 0.f : ex2(m - nm);         // (no logit yet: nothing but zeros in O)
           if (j > 0) {
             // (nobody writes O now: this page's product has not been asked for, and S arrived behind the last one's)

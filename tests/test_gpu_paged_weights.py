@@ -28,6 +28,30 @@ def refill(call, make):
         pt.store(call.pages, call.sh, [where[i] for i in keep], k[keep].astype(np.float32), v[keep].astype(np.float32))
 
 
+@pytest.mark.parametrize("peaks", ["every page", "first token", "last tokens"])
+@pytest.mark.parametrize("gap", [6.0, 13.4, 18.6, 20.6, 24.6, 28.3])
+@pytest.mark.parametrize("D", [64, 128])
+def test_flat_tail_under_peaks(kvq, D, gap, peaks):
+    """Peaks whose values are zero over a tail `gap` bits below them: the output is the tail's share alone."""
+    sh = S(D=D, kb=4, vb=4, gk=64, gv=64, G=1, Hkv=1, dtype="fp16")
+    n, rows = 900, 300
+    call = pt.Call(kvq, sh, [n], [rows], seed=1)
+    call.q = torch.ones_like(call.q)
+    t = np.arange(n)
+    at = {"every page": t % 128 == 5, "first token": t == 0, "last tokens": t >= n - rows}[peaks]
+
+    def make(_, n):
+        k = np.zeros((n, 1, D)) + np.where(at, gap / (1.4426950408889634 * D ** 0.5), 0.0)[:, None, None]
+        return k, np.ones((n, 1, D)) * ~at[:, None, None]
+    refill(call, make)
+    got, want = call.got_attention(), call.want_attention()
+    # All weights of the tail are alike, so nothing averages out.  A weight is fp16 and held at least 2^11 times as large as it is relative to
+    # the row's largest: off by 2^-11 of it, or by half of fp16's smallest step, 2^-25 2^-11 = 2^-36 of the largest weight, which is at most
+    # the sum of all.  Values are exact; fp32 sums, exponents and logits of up to 30 bits in fp32 add less than 2^-14.
+    bound = (2.0 ** -11 + 2.0 ** -14) * want + n * 2.0 ** -36
+    assert np.all(np.abs(got - want) <= bound), f"off by {(np.abs(got - want) / bound).max():.2f} of what is allowed"
+
+
 @pytest.mark.parametrize("side", ["keys", "values"])
 @pytest.mark.parametrize("sh", [S(), S(kb=8, vb=8), S(kb=2, vb=4, gk=32, gv=64), S(D=64, kb=4, vb=8, gk=64, gv=32)], ids=str)
 def test_small_values_beside_a_large_one(kvq, sh, side):
