@@ -63,7 +63,7 @@ int kvq_debug_decode_ring(const kvq_config* cfg, int32_t n_rows, int32_t* info);
  * are merged (0 for a stream without pages). */
 int kvq_debug_decode_windows(const kvq_config* cfg, int32_t n_rows, const int32_t* seq_len, int32_t* windows);
 
-/* The division that the split uses, on the device (DEVICE memory): q[i] = n[i] / d[i] for n >= 0, d > 0 and quotients below 2^31. */
+/* The division that the split uses, on the device (DEVICE memory): q[i] = n[i] / d[i] for n >= 0, d > 0 and quotients below 2^40. */
 int kvq_debug_divide(const int64_t* n, const int64_t* d, int64_t* q, int32_t count, void* cuda_stream);
 
 /* kvq_paged_attention with every device-side wait limited to wait_us microseconds (1 .. 100000) and one page withheld: the flat page
