@@ -102,6 +102,13 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
   return d;
 }
 
+// prmt.b32 with the full selector semantics (a selector nibble with bit 3 set replicates the sign of the byte).
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) {
+  uint32_t d;
+  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(sel));
+  return d;
+}
+
 // ---------------------------------------------------------------- quantizer
 struct GroupParams {
   float s, z, inv;     // fp32 values of the stored fp16 scale / zero, and 1/s (0 when s == 0)

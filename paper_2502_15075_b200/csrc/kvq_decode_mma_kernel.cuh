@@ -52,12 +52,6 @@ inline int ring_stages(const Geom& g, int nh, int ngv, bool chan, int minb, int 
 // last one beyond the rows that were copied.
 __host__ __device__ inline bool window_fits_ring(const SmemLayout& sl, int nw, int D) { return ((nw + 15) & ~15) * 4 * D <= sl.ring_bytes; }
 
-// prmt.b32 with the full selector semantics (a selector nibble with bit 3 set replicates the sign of the byte).
-__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) {
-  uint32_t d;
-  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(sel));
-  return d;
-}
 // D += A(16x32, row, unsigned bytes) * B(32x8, col, unsigned bytes), int32 accumulate.
 __device__ __forceinline__ void mma16832_u8u8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                               uint32_t b0, uint32_t b1) {

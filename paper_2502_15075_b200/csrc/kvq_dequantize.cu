@@ -6,7 +6,7 @@
 // through a padded [128][D + 8] shared tile that stmatrix fills transposed; code bytes become floats by a byte
 // permute and an exact subtraction.  Bit planes and 16-bit passthrough: the packed page is copied to shared memory
 // and expanded element by element into the tile.  Bound by the 16-bit stores (they write 4-8x what they read).
-#include "kvq_internal.h"
+#include "kvq_dequantize.cuh"
 
 namespace kvq {
 
@@ -50,23 +50,6 @@ __device__ __forceinline__ void store_rows(const uint16_t* tile, int ts, uint16_
 // code bytes of a word become floats without a conversion instruction (byte -> 0x4B0000bb = 2^23 + code, minus 2^23: exact), and
 // two elements share the subtraction, the fused multiply-add of the fixed formula and the rounding to 16 bits.
 // ---------------------------------------------------------------------------------------------------------
-// Bytes i and j of `bytes` as exact floats.
-__device__ __forceinline__ f32x2 code_pair(uint32_t bytes, int i, int j) {
-  const float a = __uint_as_float(__byte_perm(bytes, 0x4B000000u, 0x7540u + (uint32_t)i));
-  const float b = __uint_as_float(__byte_perm(bytes, 0x4B000000u, 0x7540u + (uint32_t)j));
-  return add2(pack2(a, b), pack2(-8388608.0f, -8388608.0f));
-}
-template <int DTYPE>
-__device__ __forceinline__ uint32_t pack16(f32x2 v) {
-  const float2 f = unpack2(v);
-  if constexpr (DTYPE == KVQ_FP16) {
-    const __half2 h = __floats2half2_rn(f.x, f.y);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  } else {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  }
-}
 
 // Keys of one page, straight from global memory to global memory: thread item = (token, chunk of its row); the chunk's bytes are
 // four consecutive channels of every 16-channel slice, so each slice gives one 8-byte store and the four threads of a token write 32

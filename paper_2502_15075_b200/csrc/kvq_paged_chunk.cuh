@@ -120,10 +120,10 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16]) {
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : KVQ_R8(r, 0), KVQ_R8(r, 8) : "r"(addr) : "memory");
 }
+// Waits for this thread's loads from tensor memory; the registers go through it, so that nothing is computed from them before.
 __device__ __forceinline__ void wait_ld(uint32_t (&r)[16]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : KVQ_W8(r, 0), KVQ_W8(r, 8)::"memory");
 }
-// Waits for this thread's loads from tensor memory; the registers go through it, so that nothing is computed from them before.
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -140,11 +140,6 @@ __device__ __forceinline__ uint32_t tmem_ld1(uint32_t addr) {
 }
 __device__ __forceinline__ void tmem_st1(uint32_t addr, uint32_t r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(addr), "r"(r) : "memory");
-}
-__device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t sel) {
-  uint32_t d;
-  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(sel));
-  return d;
 }
 __device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
   float d;
@@ -423,7 +418,7 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
       const int page0 = c.page, pages = c.end - c.page;
       const int pair0 = t.i * kTile + 128 * w;
       if (pair0 >= t.pairs) { it += pages; continue; }
-      // ---- the row's query: fp16 in the order of the key tiles' channels, scaled to at most 2^15 in size
+      // ---- the row's query: fp16 in the order of the key tiles' channels; rows of bf16 scaled to a largest element from 1 to below 2
       const int pair = pair0 + row, r = by_g(min(pair, t.pairs - 1));
       const bool real = pair < t.pairs;
       float f = c1;
@@ -459,8 +454,8 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
           const int i = k >> 2, ch = k & 3, a = (32 * i + 4 * ch) / 2;
-          *reinterpret_cast<uint4*>(sq + k * T::kLbQ) = make_uint4(permute(qw[a], qw[a + 1], 0x5410u), permute(qw[a], qw[a + 1], 0x7632u),
-                                                                   permute(qw[a + 8], qw[a + 9], 0x5410u), permute(qw[a + 8], qw[a + 9], 0x7632u));
+          *reinterpret_cast<uint4*>(sq + k * T::kLbQ) = make_uint4(prmt(qw[a], qw[a + 1], 0x5410u), prmt(qw[a], qw[a + 1], 0x7632u),
+                                                                   prmt(qw[a + 8], qw[a + 9], 0x5410u), prmt(qw[a + 8], qw[a + 9], 0x7632u));
         }
       }
       tc::fence_async_smem();
@@ -681,63 +676,46 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
         // the parts' places: the tile starts in the second one of its first CTA, goes on in the first one of those behind
         auto place = [&](int j) { return (size_t)(2 * (first + j) + (j == 0 ? 1 : 0)) * cap + 128 * w; };
         // a thread per 16 bytes of a row, four parts in flight at a time
-        constexpr int NP = D / 4, U = 1;
+        constexpr int NP = D / 4;
 #pragma unroll 1
-        for (int idx0 = row + 128 * side; idx0 < rows_w * NP; idx0 += 256 * U) {
-          float4 num[U];
-          float ms[U], den[U];
-          int rr[U];
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            rr[u] = min(idx0 + 256 * u, rows_w * NP - 1) / NP;
-            ms[u] = -INFINITY;
-            den[u] = 0.f;
-            num[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-          }
+        for (int idx = row + 128 * side; idx < rows_w * NP; idx += 256) {
+          const int rr = idx / NP, piece = idx & (NP - 1);
+          float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+          float ms = -INFINITY, den = 0.f;
 #pragma unroll 1
           for (int j = 0; j < parts; j += 4) {
-            float2 ml[4][U];
-            float4 o[4][U];
+            float2 ml[4];
+            float4 o[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const size_t at = place(min(j + e, parts - 1));
-#pragma unroll
-              for (int u = 0; u < U; ++u) {
-                ml[e][u] = __ldcg(mls + at + rr[u]);
-                o[e][u] = __ldcg(reinterpret_cast<const float4*>(ws + (at + rr[u]) * D) + (idx0 & (NP - 1)));
-                if (j + e >= parts) ml[e][u].x = -INFINITY;
-              }
+              const size_t at = place(min(j + e, parts - 1)) + rr;
+              ml[e] = __ldcg(mls + at);
+              o[e] = __ldcg(reinterpret_cast<const float4*>(ws + at * D) + piece);
+              if (j + e >= parts) ml[e].x = -INFINITY;
             }
+            const float mb = fmaxf(ms, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
+            if (mb == -INFINITY) continue;           // (parts without a token for this row: their o is zero, their sum too)
+            const float w0 = ms == -INFINITY ? 0.f : ex2(ms - mb);
+            den *= w0; num.x *= w0; num.y *= w0; num.z *= w0; num.w *= w0;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-              const float mb = fmaxf(ms[u], fmaxf(fmaxf(ml[0][u].x, ml[1][u].x), fmaxf(ml[2][u].x, ml[3][u].x)));
-              if (mb == -INFINITY) continue;         // (a part without a token for this row: its o is zero, its sum too)
-              const float w0 = ms[u] == -INFINITY ? 0.f : ex2(ms[u] - mb);
-              den[u] *= w0; num[u].x *= w0; num[u].y *= w0; num[u].z *= w0; num[u].w *= w0;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float wt = ml[e][u].x == -INFINITY ? 0.f : ex2(ml[e][u].x - mb);
-                den[u] = fmaf(wt, ml[e][u].y, den[u]);
-                num[u].x = fmaf(wt, o[e][u].x, num[u].x); num[u].y = fmaf(wt, o[e][u].y, num[u].y);
-                num[u].z = fmaf(wt, o[e][u].z, num[u].z); num[u].w = fmaf(wt, o[e][u].w, num[u].w);
-              }
-              ms[u] = mb;
+            for (int e = 0; e < 4; ++e) {
+              const float wt = ml[e].x == -INFINITY ? 0.f : ex2(ml[e].x - mb);
+              den = fmaf(wt, ml[e].y, den);
+              num.x = fmaf(wt, o[e].x, num.x); num.y = fmaf(wt, o[e].y, num.y);
+              num.z = fmaf(wt, o[e].z, num.z); num.w = fmaf(wt, o[e].w, num.w);
             }
+            ms = mb;
           }
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            if (idx0 + 256 * u >= rows_w * NP) break;
-            const float iv = den[u] > 0.f ? 1.0f / den[u] : 0.f;
-            const int rw = by_g(pair0 + rr[u]);
-            const size_t at = ((size_t)(t.first + rw) * g.Hq + (size_t)t.h * G + (pair0 + rr[u] - rw * G)) * D + 4 * (idx0 & (NP - 1));
-            if (out_dtype == KVQ_FP32) {
-              *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(num[u].x * iv, num[u].y * iv, num[u].z * iv, num[u].w * iv);
-            } else {
-              uint2 v;
-              v.x = (uint32_t)f32_to_bits16(num[u].x * iv, out_dtype) | ((uint32_t)f32_to_bits16(num[u].y * iv, out_dtype) << 16);
-              v.y = (uint32_t)f32_to_bits16(num[u].z * iv, out_dtype) | ((uint32_t)f32_to_bits16(num[u].w * iv, out_dtype) << 16);
-              *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = v;
-            }
+          const float iv = den > 0.f ? 1.0f / den : 0.f;
+          const int rw = by_g(pair0 + rr);
+          const size_t at = ((size_t)(t.first + rw) * g.Hq + (size_t)t.h * G + (pair0 + rr - rw * G)) * D + 4 * piece;
+          if (out_dtype == KVQ_FP32) {
+            *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(num.x * iv, num.y * iv, num.z * iv, num.w * iv);
+          } else {
+            uint2 v;
+            v.x = (uint32_t)f32_to_bits16(num.x * iv, out_dtype) | ((uint32_t)f32_to_bits16(num.y * iv, out_dtype) << 16);
+            v.y = (uint32_t)f32_to_bits16(num.z * iv, out_dtype) | ((uint32_t)f32_to_bits16(num.w * iv, out_dtype) << 16);
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = v;
           }
         }
         if (row == 0 && side == 0) counts[2 * first + w] = 0ull;
@@ -878,8 +856,8 @@ chunk_kernel(Geom g, Paged p, const uint16_t* __restrict__ q, float c1, float* _
 #pragma unroll
                   for (int pr = 0; pr < 2; ++pr) {
                     const uint32_t m0 = __shfl_sync(FULL, own, 16 * kh + 2 * tq + 8 * pr), m1 = __shfl_sync(FULL, own, 16 * kh + 2 * tq + 8 * pr + 1);
-                    s[kh][pr] = as_h2(permute(m0, m1, 0x5410u));
-                    z[kh][pr] = as_h2(permute(m0, m1, 0x7632u));
+                    s[kh][pr] = as_h2(prmt(m0, m1, 0x5410u));
+                    z[kh][pr] = as_h2(prmt(m0, m1, 0x7632u));
                   }
                 }
               }

@@ -6,6 +6,7 @@
 // are transposed by stmatrix into a padded tile of the warp's own and leave as whole rows.  Code bytes become floats by a byte
 // permute and an exact subtraction.  Bound by the 16-bit stores, which are 4 to 8 times what is read: 4 x up to 8,001 tokens of the 8B shape K4V2 27 us
 // (element by element 254), 32,768 tokens 36.6 us (161 MB, 0.67 of the copy rate).
+#include "kvq_dequantize.cuh"
 #include "kvq_paged.cuh"
 
 namespace kvq {
@@ -13,26 +14,8 @@ namespace kvq {
 namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-constexpr uint32_t FULL = 0xffffffffu;
 
 __device__ __forceinline__ float2 meta_sz(uint32_t m) { return __half22float2(*reinterpret_cast<const __half2*>(&m)); }
-// Bytes i and j of `bytes` as exact floats.
-__device__ __forceinline__ f32x2 code_pair(uint32_t bytes, int i, int j) {
-  const float a = __uint_as_float(__byte_perm(bytes, 0x4B000000u, 0x7540u + (uint32_t)i));
-  const float b = __uint_as_float(__byte_perm(bytes, 0x4B000000u, 0x7540u + (uint32_t)j));
-  return add2(pack2(a, b), pack2(-8388608.0f, -8388608.0f));
-}
-template <int DTYPE>
-__device__ __forceinline__ uint32_t pack16(f32x2 v) {
-  const float2 f = unpack2(v);
-  if constexpr (DTYPE == KVQ_FP16) {
-    const __half2 h = __floats2half2_rn(f.x, f.y);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  } else {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  }
-}
 
 // Keys of tokens lo .. hi - 1 of the block at token tp of its page.  out: the block's first token; stride: of tokens, in elements.
 template <int B, int D, int DTYPE>

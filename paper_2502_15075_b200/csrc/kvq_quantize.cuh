@@ -9,12 +9,6 @@ namespace kvq {
 constexpr uint32_t FULL = 0xffffffffu;
 constexpr float kRoundMagic = 12582912.0f;   // 1.5 * 2^23: adding it rounds to nearest-even at integer precision
 
-__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) {
-  uint32_t d;
-  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(sel));
-  return d;
-}
-
 // Two 16-bit inputs as a packed pair of their own type, for exact minima and maxima.
 template <int DTYPE> struct Pair16 { using type = __half2; };
 template <> struct Pair16<KVQ_BF16> { using type = __nv_bfloat162; };
