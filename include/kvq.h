@@ -301,7 +301,7 @@ typedef struct {
  *   k, v: device, in_dtype, element (row, head, d) at offset row * kv_stride_row + head * kv_stride_head + d (in elements; each
  *     row of head_dim channels 16-byte aligned, e.g. slices of one projection output).
  *   q, q_out: both NULL, or device, in_dtype: q with strides of its own, q_out [n_rows][n_q_heads][head_dim] contiguous.  q_out may
- *     be q where q is contiguous too.  Needs rope.
+ *     be q where q is contiguous too, and overlaps no tensor of the call otherwise.  Needs rope.
  *   rope: NULL stores the keys as they are.
  * Not safe to call concurrently on the same pages.
  */
@@ -318,8 +318,10 @@ int kvq_paged_append(const kvq_config* cfg, const kvq_paged_cache* cache, const 
  *     KVQ_FP16/BF16/FP32).
  *   max_rows: no sequence has more rows in this call (1: a decoding step; values beyond capacity_tokens count as it); sizes the workspace and chooses the kernel.  Up to
  *     n_q_heads / n_kv_heads * max_rows = 8 (row, head) pairs per KV head are served by the kernel behind kvq_decode_attention where it
- *     is built for the configuration, some more rows over long caches by several launches of it (capacity and window tell, so a
- *     capacity far above the lengths costs such calls time), everything else by one that makes 16-bit tiles of the pages for the
+ *     is built for the configuration: head_dim 128 with K4V2, K2V4, K4V4 and K8V4 in groups of 128, head_dim 64 with K4V2 in groups of
+ *     64 or of 32; up to 4 pairs also head_dim 128 with K4V2, groups of 64, or of 32 for keys and 128 for values.  Some more rows over long
+ *     caches take several launches of it (capacity and window tell, so a capacity far above the lengths costs such calls time).  Everything else,
+ *     single tokens of other widths and groups too (up to eight times the time), is served by one that makes 16-bit tiles of the pages for the
  *     tensor cores; a batch of long chunks and single tokens is faster as two calls.
  *   softmax_scale <= 0 selects 1/sqrt(head_dim).
  *   workspace: device scratch of at least kvq_paged_workspace_bytes(), 16-byte aligned, contents arbitrary.  Calls that may

@@ -3,7 +3,7 @@
 //
 // A row (one head of one token) is spread over D / 8 lanes, eight consecutive channels each: half-split pairs are a shuffle apart, interleaved
 // ones sit in a lane, and a group's minimum and maximum are a few shuffles.  8B shape with queries, K4V2: a token each for 64 sequences 3.9 us (a
-// replayed graph), prompts of 4 x 8,192 tokens 163 us for 0.70 GB (keys and queries 150 with two thirds of the issue slots, values 22).
+// replayed graph), prompts of 4 x 8,192 tokens 165 us for 0.70 GB (keys and queries 150 with two thirds of the issue slots, values 22).
 #include "kvq_paged.cuh"
 #include "kvq_quantize.cuh"
 

@@ -21,8 +21,8 @@
 // drafted rows behind a long context all fill the GPU.  A tile that falls to several CTAs leaves partials (m, l, o); the CTA that comes last
 // merges them by log-sum-exp, in a fixed order.
 //
-// 8B shape K4V2, a prompt of 8,192 tokens against its own cache 729 us (550 GFLOP: 755 TFLOP/s, 0.46 of the measured bf16 rate); two chunks of up to 700 rows
-// behind 16,001 tokens with a window of 4,096 157 us.  Bound by the chain softmax - product - softmax of a half: both products of a half
+// 8B shape K4V2, a prompt of 8,192 tokens against its own cache 749 us (550 GFLOP: 734 TFLOP/s, 0.45 of the measured bf16 rate; with a scaled token in every
+// page 924 to 949, with nothing else 2,250 to 3,420); two chunks of up to 700 rows behind 16,001 tokens with a window of 4,096 160 us.  Bound by the chain softmax - product - softmax of a half: both products of a half
 // are 1,024 cycles, its softmax about 2,000, and the other half's work covers only part of that.  (Of 830 us at one thread per row 579 were left
 // without the softmax, 733 without the conversion of pages, 494 without both.)  Not gained by: every fourth power of two by a cubic instead of the
 // special-function unit (850 against 833), the next columns loaded ahead of the arithmetic (850), products issued by a lone thread (861).

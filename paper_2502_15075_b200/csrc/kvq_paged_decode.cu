@@ -39,8 +39,8 @@ int pick_paged(const Geom& g, const Paged& p, const void* q, float c1, float* ws
 // that a SM has to read, against 13 us and 2.6 us.  Measured (8B shape, 4 heads a KV head, K4V2; launches | chunk kernel): 16 sequences x 32,767
 // tokens, 1 row 75 | 575 us, 2 rows 114 | 575, 4 rows 228 | 577, 6 rows 342 | 579, 8 rows 455 | 581; 64 x 2,000, 4 rows 90 | 194, 8 rows 180 | 199;
 // 8 x 4,096 under a window of 1,000, 2 rows 16 | 31, 4 rows 30 | 32, 6 rows 45 | 34; 1 x 32,767, 4 rows 44 | 56, 6 rows 66 | 61; 2 x 300, 2 rows 9 | 15,
-// 4 rows 18 | 16.  The lengths are not
-// known here: the capacity and the window stand for them.
+// 4 rows 18 | 16.  (The line is drawn through all of these: 1 x 32,767 with 6 rows lies on the wrong side of it.)  The lengths are not known here: the
+// capacity and the window stand for them, so that short sequences in a large capacity pay for several launches.
 int rows_per_launch(const Geom& g, const Paged& p) {
   const long long tokens = p.window > 0 && (long long)p.window + p.sinks < g.capacity ? (long long)p.window + p.sinks : g.capacity;
   const long long per_stream = (tokens + kPageTokens - 1) / kPageTokens + (tokens < g.capacity), pages = per_stream * g.B * g.Hkv;
