@@ -108,3 +108,27 @@ def test_the_largest_values_a_page_can_hold(kvq, sh):
     got, want = call.got_attention(), call.want_attention()
     assert np.all(np.isfinite(got))
     assert np.linalg.norm(got - want) / np.linalg.norm(want) <= 2e-3
+
+
+@pytest.mark.parametrize("lens,rows,window,sinks", [([700, 333], [300, 90], 0, 0), ([900, 515], [400, 200], 150, 9), ([640], [640], 129, 130), ([130, 260], [60, 260], 1, 1)])
+@pytest.mark.parametrize("sh", [S(), S(kb=8, vb=8, G=3), S(kb=2, vb=4, gk=32, gv=64, G=8, Hkv=1), S(D=64, kb=4, vb=8, gk=64, gv=32)], ids=str)
+def test_large_keys_and_values_here_and_there(kvq, sh, lens, rows, window, sinks):
+    """Tokens beyond the fp16 range on either side or both, at any place of a page, under masks and in tiles of several sequences; queries so
+    small that such a key's logits are ordinary."""
+    rng = np.random.default_rng(6)
+    call = pt.Call(kvq, sh, lens, rows, window, sinks, seed=7)
+    call.q = (call.q.float() * 2.0 ** -17).to(call.q.dtype)
+
+    def make(_, n):
+        k, v = (rng.standard_normal((n, sh.Hkv, sh.D)) for _ in range(2))
+        k *= np.where(rng.random((n, sh.Hkv)) < 0.2, 2.0 ** 17, 1.0)[..., None]
+        v *= np.where(rng.random((n, sh.Hkv)) < 0.1, 2.0 ** 17, 1.0)[..., None]
+        return k, v
+    refill(call, make)
+    got, want = call.got_attention(), call.want_attention()
+    assert np.all(np.isfinite(got))
+    # (1 + 1 + sqrt 2) 2^-11 = 1.7e-3 as above, over a sequence's rows: single outputs may be differences of large values
+    for b in range(len(lens)):
+        s = slice(call.cu[b], call.cu[b + 1])
+        assert np.linalg.norm(got[s] - want[s]) / np.linalg.norm(want[s]) <= 2e-3
+    assert np.array_equal(got, call.got_attention())
